@@ -382,6 +382,129 @@ typedef struct {
 int lf_qk_norm_rope(const void* X, const float* g, const float* cos_table, const float* sin_table,
                     const lf_producer_shape* shape, void* Y, void* hip_stream);
 
+/*
+ * Producer of Q and K with rotary positions over several axes (time, height and width of a video's or an image's tokens),
+ * and its gradients.  As lf_qk_norm_rope, with the angles made in the call: pair i of a head belongs to one axis
+ * -- the first pairs[0] pairs to axis 0, the next pairs[1] to axis 1, the others to axis 2 -- and
+ *   theta[l][i] = pos[l][axis(i)] * freq[i]     (radians; float64, reduced to a turn before it is rounded),
+ *   Y[h][l] = R(theta[l]) (X[l][h] * inv * g[h]),   inv = 1 / sqrt(mean(x^2) + eps).
+ * lf_qk_norm_rope_axes_bwd computes, for an upstream gradient dY and with z = R(-theta) dY, n = x * inv, u = z * g:
+ *   dg = sum over tokens of z * n,     dX = inv * (u - n * mean(u * n)),
+ * the mean over the channels that the norm takes.  float32 throughout, dX rounded once to bfloat16; sums in a fixed order
+ * (no atomics: results are reproducible).
+ * Arguments
+ *   X        device, bfloat16 [tokens][>= H*d], row stride x_stride_tok elements.
+ *   g        device, float32 [H*d].    pos  device, int32 [tokens][3], any values.    freq  device, float64 [d/2], finite.
+ *   Y, dY    device, bfloat16 [H][tokens][d] with the y_ strides; Y is written.
+ *   dX       device, bfloat16, written: the H*d channels of every row, with X's row stride.  It must not overlap X or dY.
+ *   dg       device, float32 [H*d], written.
+ *   workspace  device scratch of >= lf_qk_norm_rope_axes_bwd_workspace_bytes(), 256-byte aligned.
+ *   X, Y, dY, dX, g 16-byte aligned, freq 8, pos and dg 4; strides multiples of 8.  Y must not overlap X.
+ * Errors: LF_ERR_NULL, LF_ERR_SHAPE (as lf_qk_norm_rope; H*d above 16 384; pairs negative or not adding up to d/2),
+ *   LF_ERR_ALIGN, LF_ERR_WORKSPACE, LF_ERR_HIP.
+ */
+typedef struct {
+  int32_t heads;        /* H */
+  int32_t head_dim;     /* d: 64 or 128 */
+  int32_t tokens;       /* L, at most 2^30 */
+  int32_t across_heads; /* 0 / 1, as in lf_producer_shape */
+  int32_t pairing;      /* 0 interleaved, 1 half */
+  int32_t pairs[3];     /* channel pairs of each axis, d/2 in all */
+  float eps;
+  int32_t reserved;     /* set to 0 */
+  int64_t x_stride_tok; /* elements, >= H*d */
+  int64_t y_stride_tok, y_stride_head;
+} lf_axes_shape;
+
+int lf_qk_norm_rope_axes(const void* X, const float* g, const int32_t* pos, const double* freq,
+                         const lf_axes_shape* shape, void* Y, void* hip_stream);
+size_t lf_qk_norm_rope_axes_bwd_workspace_bytes(const lf_axes_shape* shape);
+int lf_qk_norm_rope_axes_bwd(const void* X, const float* g, const int32_t* pos, const double* freq,
+                             const lf_axes_shape* shape, const void* dY, void* dX, float* dg,
+                             void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Key/value cache in 4 bits.  The frames of finished chunks are only read from then on; in 4 bits they take 17/64 of their bytes.
+ * 32 neighbouring channels of a token share a scale s = 2^(byte - 127), the smallest one with max|x| <= 7 s, byte >= 1; a
+ * code is sign and magnitude (0, 0.5, 1, 1.5, 2, 3, 4, 6) of x / s, to the nearest, ties to the even code, 6 .. 7 to 6.  A group with a
+ * value that is not finite has byte 255 and reads back as NaN; magnitudes above 2.9e38 read back as infinity.
+ * The cache is one buffer of lf_kvq_bytes(), device memory of the caller, 256-byte aligned:
+ *   codes of K [H][capacity][d/2] bytes (channel 2i in the low half of byte i), codes of V likewise,
+ *   scales of K [H][capacity][d/32] bytes, scales of V,      each of the four parts padded to 256 bytes.
+ *   lf_kvq_append   writes the tokens [first, first + tokens) of every head from K and V (device, bfloat16
+ *                   [H][tokens][d] with the strides of `rows`); all other tokens stay as they are.
+ *   lf_kvq_read     the reverse: K and V are written with the values that the cache holds.
+ *   tokens = 0 enqueues nothing.
+ * Errors: LF_ERR_NULL; LF_ERR_SHAPE (head_dim not 64 or 128, heads not in 1 .. 32 767, capacity not in 1 .. 2^24, tokens outside
+ *   the cache, a row stride below d); LF_ERR_ALIGN; LF_ERR_WORKSPACE (cache missing or too small); LF_ERR_HIP.
+ */
+typedef struct {
+  int32_t heads;        /* H */
+  int32_t head_dim;     /* d: 64 or 128 */
+  int32_t capacity;     /* tokens the buffer has room for */
+  int32_t reserved;     /* set to 0 */
+} lf_kvq_shape;
+
+typedef struct {
+  int32_t first, tokens;
+  int64_t k_stride_tok, k_stride_head; /* elements; multiples of 8 */
+  int64_t v_stride_tok, v_stride_head;
+} lf_kvq_rows;
+
+size_t lf_kvq_bytes(const lf_kvq_shape* cache_shape);
+int lf_kvq_append(const void* K, const void* V, const lf_kvq_shape* cache_shape, const lf_kvq_rows* rows,
+                  void* cache, size_t cache_bytes, void* hip_stream);
+int lf_kvq_read(const void* cache, size_t cache_bytes, const lf_kvq_shape* cache_shape,
+                const lf_kvq_rows* rows, void* K, void* V, void* hip_stream);
+
+/*
+ * Blockwise sparse attention (Eq. 13) over the 4-bit cache: lf_sparse_attn with the KV tokens taken from it.
+ * Token t of the cache is token t of the path's Kcache / Vcache.  With K and V, the current chunk's tokens
+ * [kv_len - q_len, kv_len) are read from them in bfloat16 ([H][q_len][d] with the k_ and v_ strides of `shape`), as
+ * long as the chunk is being denoised, and only the history from the cache; with K and V both NULL all kv_len tokens
+ * lie in the cache (the k_ and v_ strides are not looked at).
+ * bf16 MFMA products on the values that the cache stands for, float32 softmax and accumulation, bfloat16 output.
+ * Arguments
+ *   Q, O, shape, indices, list_len, softmax_scale   as lf_sparse_attn (order of a list is free, invalid ids are skipped,
+ *              duplicates count twice, rows without a valid id are zeros).
+ *   cache, cache_shape   heads and head_dim as in `shape`, capacity at least the tokens read from it.
+ *   workspace  device scratch of >= lf_sparse_attn_kvq_workspace_bytes(), 256-byte aligned (may be NULL where that is 0).
+ *              Calls that may overlap must not share it.
+ * K and V must be finite, and so must what the cache holds for the listed blocks.
+ * Errors: as lf_sparse_attn; LF_ERR_NULL for one of K and V without the other; LF_ERR_WORKSPACE for cache or workspace.
+ */
+size_t lf_sparse_attn_kvq_workspace_bytes(const lf_shape* shape, int32_t list_len);
+int lf_sparse_attn_kvq(const void* Q, const void* cache, size_t cache_bytes, const lf_kvq_shape* cache_shape,
+                       const void* K, const void* V, const lf_shape* shape, const int32_t* indices,
+                       int32_t list_len, float softmax_scale, void* O, void* workspace,
+                       size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Attention of a few query rows (single tokens, or the query heads that share a cached head, as rows) over every token:
+ *   O_x = sum_y softmax_y(q_x . k_y * softmax_scale) v_y,   y over the first cached_len tokens of the cache and the extra_len
+ *   rows of K and V (bfloat16, [H][extra_len][d]; not looked at when extra_len = 0).  Every row sees every token.
+ * The long axis is divided among workgroups and joined in a fixed order.  Without any token the rows are zeros.
+ * workspace and the rest as lf_sparse_attn_kvq.
+ * Errors: LF_ERR_NULL; LF_ERR_SHAPE (q_len not in 1 .. 64, lengths negative or above 2^24, cached_len above the capacity, heads or head_dim
+ *   unlike the cache's); LF_ERR_ALIGN; LF_ERR_WORKSPACE; LF_ERR_HIP.
+ */
+typedef struct {
+  int32_t heads, head_dim;
+  int32_t q_len;        /* 1 .. 64 */
+  int32_t cached_len;   /* >= 0 */
+  int32_t extra_len;    /* >= 0 */
+  int32_t reserved;     /* set to 0 */
+  int64_t q_stride_tok, q_stride_head; /* elements; multiples of 8 */
+  int64_t k_stride_tok, k_stride_head;
+  int64_t v_stride_tok, v_stride_head;
+  int64_t o_stride_tok, o_stride_head;
+} lf_token_shape;
+
+size_t lf_token_attn_kvq_workspace_bytes(const lf_token_shape* shape);
+int lf_token_attn_kvq(const void* Q, const void* cache, size_t cache_bytes, const lf_kvq_shape* cache_shape,
+                      const void* K, const void* V, const lf_token_shape* shape, float softmax_scale, void* O,
+                      void* workspace, size_t workspace_bytes, void* hip_stream);
+
 /* Static, NUL-terminated description of an lf_status value. */
 const char* lf_strerror(int status);
 

@@ -26,7 +26,7 @@ def probe_lib(tag: str) -> str:
 OBJ = os.path.join(PKG, "_build")
 
 SOURCES = ["lf_host.cpp", "lf_select.hip", "lf_attn.hip", "lf_attn_wide.hip", "lf_attn_bwd.hip", "lf_attn_bwd_wide.hip", "lf_attn_bwd_q_wide.hip",
-           "lf_producer.hip"]
+           "lf_producer.hip", "lf_host_rollout.cpp", "lf_rope_axes.hip", "lf_kvq.hip", "lf_kvq_attn.hip"]
 COMMON = ["-O3", "-std=c++17", "-fPIC", "-I", os.path.join(ROOT, "include"), "-I", CSRC,
           "-Wall", "-Wno-unused-function"]
 DEVICE = ["--offload-arch=gfx950", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

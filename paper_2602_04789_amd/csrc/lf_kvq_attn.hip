@@ -1,0 +1,425 @@
+// Attention of blocks of up to 64 query rows over a cache held in 4 bits (and rows in bfloat16 behind it).
+//
+//   O_x = sum_y softmax_y(q_x . k_y scale) v_y,   y over the tokens of the listed blocks, or over all tokens
+//
+// Few query rows share the cache's bytes, so HBM bounds the call, or with a handful of blocks the chain of one wavefront.
+// Each wavefront has all rows of the block and tiles of 32 tokens of its own: the tiles of a list are dealt out over the four
+// wavefronts of `parts` workgroups, with an online softmax each and nothing shared until the end, so no barrier stands in the loop.
+//
+// The products are computed transposed, S^T = K Q^T and O^T = V^T P^T, with v_mfma_f32_16x16x32_bf16.  Their sums run over
+// channels and tokens in any order that both operands agree on.  For S^T a lane takes D/4 neighbouring channels of one token: at d = 128 a
+// whole scaled group, 16 bytes and one scale, straight from memory into the operand, through the conversions that apply the
+// scale.  For O^T a lane takes the tokens whose scores the first product left it (4 kg + {0..3} of the two halves of the tile),
+// so P stays in its registers; V goes through LDS as bfloat16 rows and comes back by the transposing read.  The bytes of
+// the next tile are requested as soon as those of the present one are converted.
+//
+// Softmax is float32 in the exp2 domain, P = exp2(s c - m), against a reference m per row that moves only when a score passes it by
+// more than 8: without that no lane asks another.  P is rounded to bfloat16 for the product (as the output is), sums of it are float32.
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "lf_rollout.h"
+
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+struct KvqAttnArgs {
+  const uint16_t *Q, *Kx, *Vx;
+  uint16_t* O;
+  const uint8_t *kc, *vc, *ks, *vs;
+  const int32_t* idx;
+  int64_t q_stride_tok, q_stride_head, k_stride_tok, k_stride_head, v_stride_tok, v_stride_head, o_stride_tok, o_stride_head;
+  int capacity, cached, extra;
+  int n, nb, n_q, n_k, nb_cached;   // lists: blocks [0, nb_cached) lie in the cache
+  int list_len, q_len, parts;
+  float c;                          // scale * log2(e)
+  float* state_o;
+  float2* state_ml;
+};
+
+constexpr int kWaves = 4;
+constexpr float kSlack = 8.0f;      // how far a score may pass the reference: P stays below 2^8
+
+#define LDS_PTR(T, p) ((__attribute__((address_space(3))) T*)(p))
+
+union Frag {
+  uint4 u;
+  uint32_t w[4];
+  bf16x2 p[4];
+  bf16x8 v;
+};
+
+// 8 codes to 8 values.
+__device__ __forceinline__ Frag decode(uint32_t code, float scale) {
+  Frag f;
+  f.p[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, scale, 0);
+  f.p[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, scale, 1);
+  f.p[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, scale, 2);
+  f.p[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, scale, 3);
+  return f;
+}
+__device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }   // 255: the conversion gives NaN
+
+// Up to 32 tokens side by side, in the cache or behind it; cnt = 0: none.
+struct Tile {
+  int tok, cnt;
+  bool ext;
+};
+
+template <int D, int NQ, bool LISTS>
+__global__ __launch_bounds__(64 * kWaves, NQ == 4 && D == 128 ? 1 : 2) void lf_kvq_attn_kernel(KvqAttnArgs a) {
+  constexpr int KS = D / 32;          // steps of the first product, 8 channels of a lane each
+  constexpr int MB = D / 16;          // tiles of 16 channels of the second
+  constexpr int CW = D / 32;          // words of codes of a lane and token (D / 4 channels)
+  constexpr int CH = D / 8;           // 16-byte chunks of a row in LDS
+  constexpr int VI = D / 64;          // scaled groups of V's tile for a lane
+  __shared__ uint4 stage[kWaves][32 * CH];
+  __shared__ float2 ml[kWaves][16 * NQ];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int col = lane & 15, kg = lane >> 4;
+  const int part = blockIdx.x % a.parts, blk = blockIdx.x / a.parts;      // blk: (head, query block)
+  const int h = LISTS ? blk / a.n_q : blk, r = LISTS ? blk % a.n_q : 0;
+  int row0 = 0, rows = a.q_len;
+  if constexpr (LISTS) {
+    const int j = r % a.nb;
+    row0 = r / a.nb * a.n + 64 * j;
+    rows = min(64, a.n - 64 * j);
+  }
+  const int64_t hrow = (int64_t)h * a.capacity;
+  const uint8_t* kc = a.kc + hrow * (D / 2);
+  const uint8_t* vc = a.vc + hrow * (D / 2);
+  const uint8_t* ks = a.ks + hrow * (D / 32);
+  const uint8_t* vs = a.vs + hrow * (D / 32);
+  const int32_t* list = LISTS ? a.idx + (int64_t)blk * a.list_len : nullptr;
+
+  Frag qf[NQ][KS];
+#pragma unroll
+  for (int q = 0; q < NQ; ++q) {
+    const int row = row0 + min(16 * q + col, rows - 1);
+    const uint16_t* p = a.Q + (int64_t)h * a.q_stride_head + (int64_t)row * a.q_stride_tok + (D / 4) * kg;
+#pragma unroll
+    for (int u = 0; u < KS; ++u) qf[q][u].u = *reinterpret_cast<const uint4*>(p + 8 * u);
+  }
+
+  // The tiles of this wavefront, in turn: entry `at` of the list (or block of 64 tokens), then its second half.
+  const int units = LISTS ? a.list_len : (a.cached + 63) / 64 + (a.extra + 63) / 64;
+  int at = part * kWaves + wave, half = 0;
+  auto next = [&]() __attribute__((always_inline)) {
+    Tile t = {0, 0, false};
+    while (at < units) {
+      int tok, cnt;
+      bool ext;
+      if constexpr (LISTS) {
+        const int id = __builtin_amdgcn_readfirstlane(list[at]);
+        ext = id >= a.nb_cached;
+        const int frame = id / a.nb, j = id - frame * a.nb;
+        tok = (ext ? frame - a.nb_cached / a.nb : frame) * a.n + 64 * j;
+        cnt = id >= 0 && id < a.n_k ? min(64, a.n - 64 * j) : 0;
+      } else {
+        const int held = (a.cached + 63) / 64;
+        ext = at >= held;
+        tok = 64 * (ext ? at - held : at);
+        cnt = min(64, (ext ? a.extra : a.cached) - tok);
+      }
+      if (cnt > 32 * half) {
+        t.tok = tok + 32 * half;
+        t.cnt = min(32, cnt - 32 * half);
+        t.ext = ext;
+        if (cnt > 32 && half == 0) half = 1;
+        else { half = 0; at += a.parts * kWaves; }
+        return t;
+      }
+      half = 0;
+      at += a.parts * kWaves;
+    }
+    return t;
+  };
+
+  uint32_t kw[2][CW], vw[VI][4], ksc[2], vsc[VI];
+  auto load = [&](const Tile& t) __attribute__((always_inline)) {
+    if (t.cnt == 0 || t.ext) return;
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const int row = t.tok + min(16 * s + col, t.cnt - 1);
+      const uint8_t* p = kc + (uint32_t)row * (D / 2) + (D / 8) * kg;
+      if constexpr (CW == 4) {
+        const uint4 x = *reinterpret_cast<const uint4*>(p);
+        kw[s][0] = x.x; kw[s][1] = x.y; kw[s][2] = x.z; kw[s][3] = x.w;
+      } else {
+        const uint2 x = *reinterpret_cast<const uint2*>(p);
+        kw[s][0] = x.x; kw[s][1] = x.y;
+      }
+      ksc[s] = ks[(uint32_t)row * (D / 32) + (D == 128 ? kg : kg >> 1)];
+    }
+#pragma unroll
+    for (int i = 0; i < VI; ++i) {
+      const int item = 64 * i + lane, row = t.tok + min(item / (D / 32), t.cnt - 1), grp = item % (D / 32);
+      const uint4 x = *reinterpret_cast<const uint4*>(vc + (uint32_t)row * (D / 2) + 16 * grp);
+      vw[i][0] = x.x; vw[i][1] = x.y; vw[i][2] = x.z; vw[i][3] = x.w;
+      vsc[i] = vs[(uint32_t)row * (D / 32) + grp];
+    }
+  };
+
+  f32x4 oacc[NQ][MB];
+  float m_run[NQ], l_run[NQ];
+#pragma unroll
+  for (int q = 0; q < NQ; ++q) {
+    m_run[q] = -INFINITY;
+    l_run[q] = 0.0f;
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb) oacc[q][mb] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  }
+  // Rows of V in LDS: the transposing read takes 32 bytes of four rows at a time, which land in different banks when the row's two low bits
+  // go to the chunk's high bits (d = 128) or its second bit does (d = 64).
+  auto swz = [](int row, int ch) __attribute__((always_inline)) { return CH == 16 ? ch ^ ((row & 3) << 2) : ch ^ (((row >> 1) & 1) << 2); };
+  uint4* vt = stage[wave];
+
+  Tile cur = next();
+  load(cur);
+  while (cur.cnt > 0) {
+    Frag kf[2][KS];
+    if (!cur.ext) {
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int u = 0; u < KS; ++u) kf[s][u] = decode(kw[s][u], scale_of(ksc[s]));
+#pragma unroll
+      for (int i = 0; i < VI; ++i) {
+        const int item = 64 * i + lane, row = item / (D / 32), grp = item % (D / 32);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) vt[row * CH + swz(row, 4 * grp + u)] = decode(vw[i][u], scale_of(vsc[i])).u;
+      }
+    } else {
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        const int row = cur.tok + min(16 * s + col, cur.cnt - 1);
+        const uint16_t* p = a.Kx + (int64_t)h * a.k_stride_head + (int64_t)row * a.k_stride_tok + (D / 4) * kg;
+#pragma unroll
+        for (int u = 0; u < KS; ++u) kf[s][u].u = *reinterpret_cast<const uint4*>(p + 8 * u);
+      }
+#pragma unroll
+      for (int i = 0; i < VI; ++i) {
+        const int item = 64 * i + lane, row = item / (D / 32), grp = item % (D / 32);
+        const uint16_t* p = a.Vx + (int64_t)h * a.v_stride_head + (int64_t)(cur.tok + min(row, cur.cnt - 1)) * a.v_stride_tok + 32 * grp;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) vt[row * CH + swz(row, 4 * grp + u)] = *reinterpret_cast<const uint4*>(p + 8 * u);
+      }
+    }
+    const Tile then = next();
+    load(then);
+
+    f32x4 sacc[NQ][2];
+#pragma unroll
+    for (int q = 0; q < NQ; ++q)
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        sacc[q][s] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int u = 0; u < KS; ++u) sacc[q][s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[s][u].v, qf[q][u].v, sacc[q][s], 0, 0, 0);
+      }
+    bf16x8 pf[NQ];
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) {
+      float s[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s[i] = sacc[q][i >> 2][i & 3] * a.c;
+      if (cur.cnt < 32) {       // (the tile's last tokens are there twice)
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (16 * (i >> 2) + 4 * kg + (i & 3) >= cur.cnt) s[i] = -INFINITY;
+      }
+      float top = s[0];
+#pragma unroll
+      for (int i = 1; i < 8; ++i) top = fmaxf(top, s[i]);
+      if (__ballot(top > m_run[q] + kSlack) != 0ull) {
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float m_new = fmaxf(m_run[q], top);
+        // a row without a finite score yet keeps its sums of zero
+        const float alpha = m_new == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m_run[q] - m_new);
+        m_run[q] = m_new;
+        l_run[q] *= alpha;
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) oacc[q][mb][i] *= alpha;
+      }
+      const float m = m_run[q] == -INFINITY ? 0.0f : m_run[q];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float p = __builtin_amdgcn_exp2f(s[i] - m);
+        l_run[q] += p;
+        pf[q][i] = (__bf16)p;
+      }
+    }
+    // this wavefront's own rows: LDS keeps its order, and the compiler its own
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+    const uint16_t* v16 = reinterpret_cast<const uint16_t*>(vt);
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb) {
+      const int vrow = 4 * kg + (col >> 2), vcol = 16 * mb + 4 * (col & 3);
+      const int off = (vrow * CH + swz(vrow, vcol >> 3)) * 8 + (vcol & 7);      // (16 rows on the swizzle is the same)
+      const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(LDS_PTR(bf16x4, v16 + off));
+      const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(LDS_PTR(bf16x4, v16 + off + 16 * CH * 8));
+      const bf16x8 vf = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+#pragma unroll
+      for (int q = 0; q < NQ; ++q) oacc[q][mb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[q], oacc[q][mb], 0, 0, 0);
+    }
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+    cur = then;
+  }
+
+  // The four wavefronts' states become one.
+#pragma unroll
+  for (int q = 0; q < NQ; ++q) {
+    l_run[q] += __shfl_xor(l_run[q], 16);
+    l_run[q] += __shfl_xor(l_run[q], 32);
+    if (kg == 0) ml[wave][16 * q + col] = make_float2(m_run[q], l_run[q]);
+  }
+  __syncthreads();
+  f32x4* buf = reinterpret_cast<f32x4*>(&stage[0][0]);        // MB tiles of four wavefronts, 64 lanes each: the whole stage
+#pragma unroll
+  for (int q = 0; q < NQ; ++q) {
+    float M = -INFINITY, L = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) M = fmaxf(M, ml[w][16 * q + col].x);
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const float2 x = ml[w][16 * q + col];
+      L += x.x == -INFINITY ? 0.0f : x.y * __builtin_amdgcn_exp2f(x.x - M);
+    }
+    const float f = m_run[q] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m_run[q] - M);
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb) {
+      f32x4 o = oacc[q][mb];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[i] *= f;
+      buf[(mb * kWaves + wave) * 64 + lane] = o;
+    }
+    __syncthreads();
+    const int row = 16 * q + col;
+#pragma unroll
+    for (int k = 0; k < MB / kWaves; ++k) {
+      const int mb = k * kWaves + wave;
+      f32x4 o = buf[mb * kWaves * 64 + lane];
+#pragma unroll
+      for (int w = 1; w < kWaves; ++w) {
+        const f32x4 x = buf[(mb * kWaves + w) * 64 + lane];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] += x[i];
+      }
+      if (a.parts == 1) {
+        if (row < rows) {
+          const float inv = L > 0.0f || L != L ? 1.0f / L : 0.0f;        // no token at all: zeros
+          bf16x4 y;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) y[i] = (__bf16)(o[i] * inv);
+          *reinterpret_cast<bf16x4*>(a.O + (int64_t)h * a.o_stride_head + (int64_t)(row0 + row) * a.o_stride_tok + 16 * mb + 4 * kg) = y;
+        }
+      } else {
+        *reinterpret_cast<f32x4*>(a.state_o + (((int64_t)blockIdx.x * 16 * NQ + row) * D + 16 * mb + 4 * kg)) = o;
+      }
+    }
+    if (a.parts > 1 && wave == 0 && kg == 0) a.state_ml[(int64_t)blockIdx.x * 16 * NQ + row] = make_float2(M, L);
+    __syncthreads();
+  }
+}
+
+// Joins the parts of a row: a wavefront each, lane p holding part p's weight.
+template <int D>
+__global__ __launch_bounds__(256) void lf_kvq_join_kernel(KvqAttnArgs a, int rows_max, int tile_rows, int H) {
+  constexpr int W = D / 64;       // channels of a lane
+  const int lane = threadIdx.x & 63;
+  const int64_t row = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int blk = (int)(row / rows_max), i = (int)(row % rows_max);
+  if (blk >= H * a.n_q) return;
+  const int h = blk / a.n_q, r = blk % a.n_q;
+  int row0 = 0, rows = a.q_len;
+  if (a.idx) {
+    const int j = r % a.nb;
+    row0 = r / a.nb * a.n + 64 * j;
+    rows = min(64, a.n - 64 * j);
+  }
+  if (i >= rows) return;
+  const int64_t first = (int64_t)blk * a.parts * tile_rows + i;      // row of part 0; the others tile_rows apart
+  float2 x = make_float2(-INFINITY, 0.0f);
+  if (lane < a.parts) x = a.state_ml[first + (int64_t)lane * tile_rows];
+  float M = x.x;
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) M = fmaxf(M, __shfl_xor(M, off));
+  const float wgt = x.x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(x.x - M);
+  float L = wgt == 0.0f ? 0.0f : wgt * x.y;
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) L += __shfl_xor(L, off);
+  const float inv = L > 0.0f || L != L ? 1.0f / L : 0.0f;
+  float o[W];
+#pragma unroll
+  for (int e = 0; e < W; ++e) o[e] = 0.0f;
+#pragma unroll 4
+  for (int p = 0; p < a.parts; ++p) {
+    const float w = __shfl(wgt, p);
+    const float* from = a.state_o + (first + (int64_t)p * tile_rows) * D + W * lane;
+#pragma unroll
+    for (int e = 0; e < W; ++e) o[e] = fmaf(w, from[e], o[e]);
+  }
+  uint16_t* to = a.O + (int64_t)h * a.o_stride_head + (int64_t)(row0 + i) * a.o_stride_tok + W * lane;
+#pragma unroll
+  for (int e = 0; e < W; ++e) reinterpret_cast<__bf16*>(to)[e] = (__bf16)(o[e] * inv);
+}
+
+template <int D, bool LISTS>
+void (*attn_kernel(int tiles))(KvqAttnArgs) {
+  return tiles == 1 ? lf_kvq_attn_kernel<D, 1, LISTS> : tiles == 2 ? lf_kvq_attn_kernel<D, 2, LISTS> : lf_kvq_attn_kernel<D, 4, LISTS>;
+}
+
+}  // namespace
+
+int lf_launch_kvq_attn(const lf_kvq_call* c, void* stream) {
+  const lf_kvq_parts p = lf_kvq_layout(c->cs);
+  KvqAttnArgs a = {};
+  a.Q = (const uint16_t*)c->Q;
+  a.Kx = (const uint16_t*)c->K;
+  a.Vx = (const uint16_t*)c->V;
+  a.O = (uint16_t*)c->O;
+  a.kc = c->cache + p.codes[0];
+  a.vc = c->cache + p.codes[1];
+  a.ks = c->cache + p.scales[0];
+  a.vs = c->cache + p.scales[1];
+  a.idx = c->indices;
+  a.q_stride_tok = c->q_stride_tok; a.q_stride_head = c->q_stride_head;
+  a.k_stride_tok = c->k_stride_tok; a.k_stride_head = c->k_stride_head;
+  a.v_stride_tok = c->v_stride_tok; a.v_stride_head = c->v_stride_head;
+  a.o_stride_tok = c->o_stride_tok; a.o_stride_head = c->o_stride_head;
+  a.capacity = c->cs.capacity;
+  a.cached = c->cached;
+  a.extra = c->extra;
+  a.n = c->n; a.nb = c->nb; a.n_q = c->n_q; a.n_k = c->n_k;
+  a.nb_cached = c->indices ? c->cached / c->n * c->nb : 0;
+  a.list_len = c->list_len;
+  a.q_len = c->q_len;
+  a.parts = c->parts;
+  a.c = c->scale * 1.44269504088896340736f;
+  const int tiles = lf_kvq_tiles(c->rows);
+  const int64_t blocks = (int64_t)c->H * c->n_q;
+  a.state_o = (float*)c->workspace;
+  a.state_ml = (float2*)((float*)c->workspace + blocks * c->parts * 16 * tiles * c->d);
+  hipStream_t st = (hipStream_t)stream;
+  auto kernel = c->d == 128 ? (c->indices ? attn_kernel<128, true>(tiles) : attn_kernel<128, false>(tiles))
+                            : (c->indices ? attn_kernel<64, true>(tiles) : attn_kernel<64, false>(tiles));
+  hipError_t rc = lf_launch(kernel, dim3((unsigned)(blocks * c->parts)), dim3(64 * kWaves), 0, st, a);
+  if (rc != hipSuccess) return LF_ERR_HIP;
+  if (c->parts == 1) return LF_OK;
+  const unsigned grid = (unsigned)((blocks * c->rows + 3) / 4);
+  rc = c->d == 128 ? lf_launch(lf_kvq_join_kernel<128>, dim3(grid), dim3(256), 0, st, a, c->rows, 16 * tiles, c->H)
+                   : lf_launch(lf_kvq_join_kernel<64>, dim3(grid), dim3(256), 0, st, a, c->rows, 16 * tiles, c->H);
+  return rc == hipSuccess ? LF_OK : LF_ERR_HIP;
+}

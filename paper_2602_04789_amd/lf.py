@@ -56,6 +56,31 @@ class lf_producer_shape(C.Structure):
                 ("x_stride_tok", C.c_int64), ("y_stride_tok", C.c_int64), ("y_stride_head", C.c_int64)]
 
 
+class lf_axes_shape(C.Structure):
+    _fields_ = [("heads", C.c_int32), ("head_dim", C.c_int32), ("tokens", C.c_int32),
+                ("across_heads", C.c_int32), ("pairing", C.c_int32), ("pairs", C.c_int32 * 3),
+                ("eps", C.c_float), ("reserved", C.c_int32),
+                ("x_stride_tok", C.c_int64), ("y_stride_tok", C.c_int64), ("y_stride_head", C.c_int64)]
+
+
+class lf_kvq_shape(C.Structure):
+    _fields_ = [("heads", C.c_int32), ("head_dim", C.c_int32), ("capacity", C.c_int32), ("reserved", C.c_int32)]
+
+
+class lf_kvq_rows(C.Structure):
+    _fields_ = [("first", C.c_int32), ("tokens", C.c_int32), ("k_stride_tok", C.c_int64), ("k_stride_head", C.c_int64),
+                ("v_stride_tok", C.c_int64), ("v_stride_head", C.c_int64)]
+
+
+class lf_token_shape(C.Structure):
+    _fields_ = [("heads", C.c_int32), ("head_dim", C.c_int32), ("q_len", C.c_int32), ("cached_len", C.c_int32),
+                ("extra_len", C.c_int32), ("reserved", C.c_int32),
+                ("q_stride_tok", C.c_int64), ("q_stride_head", C.c_int64),
+                ("k_stride_tok", C.c_int64), ("k_stride_head", C.c_int64),
+                ("v_stride_tok", C.c_int64), ("v_stride_head", C.c_int64),
+                ("o_stride_tok", C.c_int64), ("o_stride_head", C.c_int64)]
+
+
 class LfError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -105,6 +130,28 @@ def load() -> C.CDLL:
     lib.lf_sparse_attn_bwd.restype = C.c_int
     lib.lf_qk_norm_rope.argtypes = [vp, vp, vp, vp, C.POINTER(lf_producer_shape), vp, vp]
     lib.lf_qk_norm_rope.restype = C.c_int
+    axp, kvp, rwp, tkp = (C.POINTER(t) for t in (lf_axes_shape, lf_kvq_shape, lf_kvq_rows, lf_token_shape))
+    lib.lf_qk_norm_rope_axes.argtypes = [vp, vp, vp, vp, axp, vp, vp]
+    lib.lf_qk_norm_rope_axes.restype = C.c_int
+    lib.lf_qk_norm_rope_axes_bwd_workspace_bytes.argtypes = [axp]
+    lib.lf_qk_norm_rope_axes_bwd_workspace_bytes.restype = C.c_size_t
+    lib.lf_qk_norm_rope_axes_bwd.argtypes = [vp, vp, vp, vp, axp, vp, vp, vp, vp, C.c_size_t, vp]
+    lib.lf_qk_norm_rope_axes_bwd.restype = C.c_int
+    lib.lf_kvq_bytes.argtypes = [kvp]
+    lib.lf_kvq_bytes.restype = C.c_size_t
+    lib.lf_kvq_append.argtypes = [vp, vp, kvp, rwp, vp, C.c_size_t, vp]
+    lib.lf_kvq_append.restype = C.c_int
+    lib.lf_kvq_read.argtypes = [vp, C.c_size_t, kvp, rwp, vp, vp, vp]
+    lib.lf_kvq_read.restype = C.c_int
+    lib.lf_sparse_attn_kvq_workspace_bytes.argtypes = [C.POINTER(lf_shape), C.c_int32]
+    lib.lf_sparse_attn_kvq_workspace_bytes.restype = C.c_size_t
+    lib.lf_sparse_attn_kvq.argtypes = [vp, vp, C.c_size_t, kvp, vp, vp, C.POINTER(lf_shape), vp, C.c_int32, C.c_float, vp, vp,
+                                       C.c_size_t, vp]
+    lib.lf_sparse_attn_kvq.restype = C.c_int
+    lib.lf_token_attn_kvq_workspace_bytes.argtypes = [tkp]
+    lib.lf_token_attn_kvq_workspace_bytes.restype = C.c_size_t
+    lib.lf_token_attn_kvq.argtypes = [vp, vp, C.c_size_t, kvp, vp, vp, tkp, C.c_float, vp, vp, C.c_size_t, vp]
+    lib.lf_token_attn_kvq.restype = C.c_int
     lib.lf_kcache_bytes.argtypes = [C.POINTER(lf_shape), C.c_int32]
     lib.lf_kcache_bytes.restype = C.c_size_t
     lib.lf_kcache_update.argtypes = [vp, C.POINTER(lf_shape), C.c_int32, C.c_int32, C.c_int32, vp,
@@ -469,3 +516,251 @@ def lf_qk_norm_rope(X, g, cos_table, sin_table, heads: int, Y, eps: float = 1e-6
     if rc != LF_OK:
         raise LfError(rc, "lf_qk_norm_rope")
     return Y
+
+
+def _one_device(stream, *tensors):
+    """All tensors on the current device (where the launch goes), and the stream too."""
+    at = (_torch or _get_torch()).cuda.current_device()
+    for t in tensors:
+        if t is not None and t.device.index != at:
+            raise ValueError("all tensors must live on the current device")
+    if stream is not None and getattr(stream, "device_index", at) != at:
+        raise ValueError("stream must belong to the current device")
+
+
+def _new(shape, dtype, like, stream):
+    """A tensor for work on `stream`: taken from that stream's memory, so nothing else still uses it there."""
+    torch = _torch or _get_torch()
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=like.device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=like.device)
+
+
+def _rows_strides(t, name: str):
+    """Token and head stride of a [H, L, d] tensor; those of an axis of length one do not matter."""
+    st, sh = _strides(t, name), t.shape
+    return (sh[2] if sh[1] == 1 else st[1]), (0 if sh[0] == 1 else st[0])
+
+
+def _check_buffer(t, name: str):
+    if t.dtype != (_torch or _get_torch()).uint8 or not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous uint8 GPU tensor")
+
+
+def _workspace(workspace, need: int, like, stream):
+    """(pointer, bytes) of the caller's scratch or of a new one, and the tensor, to be held until the call returns."""
+    if workspace is None:
+        if need == 0:
+            return 0, 0, None
+        workspace = _new(need, (_torch or _get_torch()).uint8, like, stream)
+    else:
+        _one_device(None, workspace)
+        if not workspace.is_contiguous():
+            raise ValueError("workspace must be contiguous")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
+
+
+def _axes_shape(X, g, pos, freq, pairs, heads, d, eps, across_heads, pairing, xs, yst, ysh) -> lf_axes_shape:
+    torch = _torch or _get_torch()
+    for t, dt, name in ((g, torch.float32, "g must be float32 [H * d]"), (pos, torch.int32, "pos must be int32 [L, 3]"),
+                        (freq, torch.float64, "freq must be float64 [d / 2]")):
+        if t.dtype != dt or not t.is_cuda or not t.is_contiguous():
+            raise ValueError(name + ", a contiguous GPU tensor")
+    if X.shape[1] < heads * d or g.numel() != heads * d or pos.shape != (X.shape[0], 3) or freq.numel() != d // 2:
+        raise ValueError("shapes of X, g, pos or freq do not fit")
+    if len(pairs) != 3:
+        raise ValueError("pairs holds the channel pairs of three axes")
+    return lf_axes_shape(heads, d, X.shape[0], int(bool(across_heads)), int(pairing), (C.c_int32 * 3)(*pairs), float(eps), 0,
+                         heads * d if X.shape[0] == 1 else xs, yst, ysh)
+
+
+def _check_rows(t, name: str, dims: int):
+    if t.dtype != (_torch or _get_torch()).bfloat16 or not t.is_cuda or t.dim() != dims or t.stride(-1) != 1:
+        raise ValueError(f"{name} must be a bfloat16 GPU tensor of {dims} axes with contiguous channels")
+
+
+def lf_qk_norm_rope_axes(X, g, pos, freq, pairs, heads: int, Y, eps: float = 1e-6, across_heads: bool = False,
+                         pairing: int = 0, stream=None):
+    """RMSNorm and rotary positions over three axes of the token-major activation X [L, >= H*d] (bfloat16) into the head-major
+    tensor Y [H, L, d] (bfloat16; may be a view into Q or into the K cache).  ``pos`` int32 [L, 3] (time, height, width),
+    ``freq`` float64 [d/2] in radians per position, ``pairs`` how many channel pairs each axis has."""
+    _check_rows(X, "X", 2)
+    yt, yh = _rows_strides(Y, "Y")
+    heads, (yheads, tokens, d) = int(heads), Y.shape
+    if yheads != heads or tokens != X.shape[0]:
+        raise ValueError("Y must be [H, L, d]")
+    p = _axes_shape(X, g, pos, freq, pairs, heads, d, eps, across_heads, pairing, X.stride(0), yt, yh)
+    _one_device(stream, X, g, pos, freq, Y)
+    rc = (_lib or load()).lf_qk_norm_rope_axes(X.data_ptr(), g.data_ptr(), pos.data_ptr(), freq.data_ptr(), C.byref(p),
+                                               Y.data_ptr(), _stream_ptr(stream))
+    if rc != LF_OK:
+        raise LfError(rc, "lf_qk_norm_rope_axes")
+    return Y
+
+
+def lf_qk_norm_rope_axes_bwd_workspace_bytes(heads: int, head_dim: int, tokens: int) -> int:
+    p = lf_axes_shape(heads, head_dim, tokens, 0, 0, (C.c_int32 * 3)(head_dim // 2, 0, 0), 0.0, 0, heads * head_dim, head_dim,
+                      tokens * head_dim)
+    return int(load().lf_qk_norm_rope_axes_bwd_workspace_bytes(C.byref(p)))
+
+
+def lf_qk_norm_rope_axes_bwd(X, g, pos, freq, pairs, heads: int, dY, eps: float = 1e-6, across_heads: bool = False,
+                             pairing: int = 0, workspace=None, stream=None, grads=None):
+    """Gradients of lf_qk_norm_rope_axes for an upstream gradient dY [H, L, d] (bfloat16); returns (dX, dg): dX bfloat16 with the
+    shape and row stride of X, of which the first H*d channels are written, dg float32 [H*d] (``grads``: two such tensors to
+    write into instead of new ones)."""
+    torch = _torch or _get_torch()
+    _check_rows(X, "X", 2)
+    yt, yh = _rows_strides(dY, "dY")
+    heads, (yheads, tokens, d) = int(heads), dY.shape
+    if yheads != heads or tokens != X.shape[0]:
+        raise ValueError("dY must be [H, L, d]")
+    p = _axes_shape(X, g, pos, freq, pairs, heads, d, eps, across_heads, pairing, X.stride(0), yt, yh)
+    if grads is None:
+        dg = _new((heads * d,), torch.float32, X, stream)
+        if tokens == 1 or X.stride(0) == X.shape[1]:
+            dX = _new(tuple(X.shape), torch.bfloat16, X, stream)
+        else:
+            dX = _new((tokens * X.stride(0),), torch.bfloat16, X, stream).as_strided(X.shape, X.stride())
+    else:
+        dX, dg = grads
+        _check_rows(dX, "dX", 2)
+        if dX.shape != X.shape or (tokens > 1 and dX.stride(0) != X.stride(0)):
+            raise ValueError("dX must have the shape and strides of X")
+        if dg.dtype != torch.float32 or not dg.is_contiguous() or dg.numel() != heads * d:
+            raise ValueError("dg must be a contiguous float32 GPU tensor [H * d]")
+    _one_device(stream, X, g, pos, freq, dY, dX, dg)
+    lib = _lib or load()
+    ws, nbytes, _keep = _workspace(workspace, 0 if workspace is not None else
+                                   int(lib.lf_qk_norm_rope_axes_bwd_workspace_bytes(C.byref(p))), X, stream)
+    rc = lib.lf_qk_norm_rope_axes_bwd(X.data_ptr(), g.data_ptr(), pos.data_ptr(), freq.data_ptr(), C.byref(p), dY.data_ptr(),
+                                      dX.data_ptr(), dg.data_ptr(), ws, nbytes, _stream_ptr(stream))
+    if rc != LF_OK:
+        raise LfError(rc, "lf_qk_norm_rope_axes_bwd")
+    return dX, dg
+
+
+def lf_kvq_bytes(heads: int, head_dim: int, capacity: int) -> int:
+    """Bytes of a 4-bit cache for `capacity` tokens (0 on bad input)."""
+    return int(load().lf_kvq_bytes(C.byref(lf_kvq_shape(heads, head_dim, capacity, 0))))
+
+
+def lf_kvq_append(K, V, cache, capacity: int, first: int, stream=None):
+    """Write the tokens [first, first + L) of the 4-bit cache from K and V [H, L, d] (bfloat16); returns ``cache`` (a uint8
+    device tensor of >= lf_kvq_bytes())."""
+    (kt, kh), (vt, vh) = _rows_strides(K, "K"), _rows_strides(V, "V")
+    _check_buffer(cache, "cache")
+    if K.shape != V.shape:
+        raise ValueError("K and V must have one shape")
+    heads, tokens, d = K.shape
+    _one_device(stream, K, V, cache)
+    rc = (_lib or load()).lf_kvq_append(K.data_ptr(), V.data_ptr(), C.byref(lf_kvq_shape(heads, d, int(capacity), 0)),
+                                        C.byref(lf_kvq_rows(int(first), tokens, kt, kh, vt, vh)), cache.data_ptr(), cache.numel(),
+                                        _stream_ptr(stream))
+    if rc != LF_OK:
+        raise LfError(rc, "lf_kvq_append")
+    return cache
+
+
+def lf_kvq_read(cache, heads: int, head_dim: int, capacity: int, first: int, tokens: int, K=None, V=None, stream=None):
+    """The values that tokens [first, first + tokens) of the 4-bit cache stand for: (K, V), bfloat16 [H, tokens, d]."""
+    torch = _torch or _get_torch()
+    _check_buffer(cache, "cache")
+    shape = (int(heads), int(tokens), int(head_dim))
+    if K is None:
+        K = _new(shape, torch.bfloat16, cache, stream)
+    if V is None:
+        V = _new(shape, torch.bfloat16, cache, stream)
+    (kt, kh), (vt, vh) = _rows_strides(K, "K"), _rows_strides(V, "V")
+    if tuple(K.shape) != shape or tuple(V.shape) != shape:
+        raise ValueError("K and V must be [H, tokens, d]")
+    _one_device(stream, cache, K, V)
+    rc = (_lib or load()).lf_kvq_read(cache.data_ptr(), cache.numel(), C.byref(lf_kvq_shape(shape[0], shape[2], int(capacity), 0)),
+                                      C.byref(lf_kvq_rows(int(first), shape[1], kt, kh, vt, vh)), K.data_ptr(), V.data_ptr(),
+                                      _stream_ptr(stream))
+    if rc != LF_OK:
+        raise LfError(rc, "lf_kvq_read")
+    return K, V
+
+
+def lf_sparse_attn_kvq_workspace_bytes(heads: int, head_dim: int, frame_len: int, block: int, q_len: int, kv_len: int,
+                                       list_len: int) -> int:
+    d = int(head_dim)
+    sh = lf_shape(heads, d, frame_len, block, q_len, kv_len, LF_BF16, 0, d, 0, d, 0, d, 0, d, 0)
+    return int(load().lf_sparse_attn_kvq_workspace_bytes(C.byref(sh), list_len))
+
+
+def lf_sparse_attn_kvq(Q, cache, capacity: int, kv_len: int, indices, frame_len: int, block: int, K=None, V=None,
+                       softmax_scale: float = 0.0, O=None, workspace=None, stream=None):
+    """Blockwise sparse attention over the 4-bit cache; returns O (bfloat16 [H, q_len, d], device).  With ``K`` and ``V`` [H, q_len,
+    d] the current chunk's tokens, the last q_len of kv_len, are read from them in bfloat16, without them from the cache."""
+    torch = _torch or _get_torch()
+    if (K is None) != (V is None):
+        raise ValueError("K and V go together")
+    _check_buffer(cache, "cache")
+    qt, qh = _rows_strides(Q, "Q")
+    heads, q_len, d = Q.shape
+    kt = kh = vt = vh = 0
+    if K is not None:
+        (kt, kh), (vt, vh) = _rows_strides(K, "K"), _rows_strides(V, "V")
+        if K.shape != Q.shape or V.shape != Q.shape:
+            raise ValueError("K and V must be [H, q_len, d], the current chunk's tokens")
+    if O is None:
+        O = _new((heads, q_len, d), torch.bfloat16, Q, stream)
+    ot, oh = _rows_strides(O, "O")
+    if O.shape != Q.shape:
+        raise ValueError("O must be [H, q_len, d]")
+    sh = lf_shape(heads, d, int(frame_len), int(block), q_len, int(kv_len), LF_BF16, 0, qt, qh, kt, kh, vt, vh, ot, oh)
+    _check_lists(indices, sh, frame_len)
+    _one_device(stream, Q, cache, indices, K, V, O)
+    lib = _lib or load()
+    ws, nbytes, _keep = _workspace(workspace, 0 if workspace is not None else
+                                   int(lib.lf_sparse_attn_kvq_workspace_bytes(C.byref(sh), indices.shape[2])), Q, stream)
+    rc = lib.lf_sparse_attn_kvq(Q.data_ptr(), cache.data_ptr(), cache.numel(), C.byref(lf_kvq_shape(heads, d, int(capacity), 0)),
+                                None if K is None else K.data_ptr(), None if V is None else V.data_ptr(), C.byref(sh),
+                                indices.data_ptr(), indices.shape[2], float(softmax_scale), O.data_ptr(), ws, nbytes,
+                                _stream_ptr(stream))
+    if rc != LF_OK:
+        raise LfError(rc, "lf_sparse_attn_kvq")
+    return O
+
+
+def lf_token_attn_kvq_workspace_bytes(heads: int, head_dim: int, q_len: int, cached_len: int, extra_len: int) -> int:
+    d = int(head_dim)
+    sh = lf_token_shape(heads, d, q_len, cached_len, extra_len, 0, d, 0, d, 0, d, 0, d, 0)
+    return int(load().lf_token_attn_kvq_workspace_bytes(C.byref(sh)))
+
+
+def lf_token_attn_kvq(Q, cache, capacity: int, cached_len: int, K=None, V=None, softmax_scale: float = 0.0, O=None,
+                      workspace=None, stream=None):
+    """Attention of up to 64 query rows [H, q_len, d] over the first ``cached_len`` tokens of the 4-bit cache and the tokens of ``K``
+    and ``V`` [H, extra, d] (bfloat16, optional) behind them; returns O (bfloat16 [H, q_len, d], device)."""
+    torch = _torch or _get_torch()
+    if (K is None) != (V is None):
+        raise ValueError("K and V go together")
+    _check_buffer(cache, "cache")
+    qt, qh = _rows_strides(Q, "Q")
+    heads, q_len, d = Q.shape
+    extra = kt = kh = vt = vh = 0
+    if K is not None:
+        (kt, kh), (vt, vh) = _rows_strides(K, "K"), _rows_strides(V, "V")
+        extra = K.shape[1]
+        if K.shape != V.shape or K.shape[0] != heads or K.shape[2] != d:
+            raise ValueError("K and V must be [H, extra, d]")
+    if O is None:
+        O = _new((heads, q_len, d), torch.bfloat16, Q, stream)
+    ot, oh = _rows_strides(O, "O")
+    if O.shape != Q.shape:
+        raise ValueError("O must be [H, q_len, d]")
+    sh = lf_token_shape(heads, d, q_len, int(cached_len), extra, 0, qt, qh, kt, kh, vt, vh, ot, oh)
+    _one_device(stream, Q, cache, K, V, O)
+    lib = _lib or load()
+    ws, nbytes, _keep = _workspace(workspace, 0 if workspace is not None else
+                                   int(lib.lf_token_attn_kvq_workspace_bytes(C.byref(sh))), Q, stream)
+    rc = lib.lf_token_attn_kvq(Q.data_ptr(), cache.data_ptr(), cache.numel(), C.byref(lf_kvq_shape(heads, d, int(capacity), 0)),
+                               None if K is None else K.data_ptr(), None if V is None else V.data_ptr(), C.byref(sh),
+                               float(softmax_scale), O.data_ptr(), ws, nbytes, _stream_ptr(stream))
+    if rc != LF_OK:
+        raise LfError(rc, "lf_token_attn_kvq")
+    return O
