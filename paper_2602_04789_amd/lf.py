@@ -518,14 +518,27 @@ def lf_qk_norm_rope(X, g, cos_table, sin_table, heads: int, Y, eps: float = 1e-6
     return Y
 
 
-def _one_device(stream, *tensors):
-    """All tensors on the current device (where the launch goes), and the stream too."""
-    at = (_torch or _get_torch()).cuda.current_device()
+def _here(stream):
+    """(current device, pointer of the stream): where a launch goes."""
+    torch = _torch or _get_torch()
+    if stream is not None:
+        at = torch.cuda.current_device()
+        if getattr(stream, "device_index", at) != at:
+            raise ValueError("stream must belong to the current device")
+        return at, int(stream.cuda_stream)
+    # as _stream_ptr, and without torch.cuda's look at its own state (0.5 us for both)
+    try:
+        at = torch._C._cuda_getDevice()
+        return at, torch._C._cuda_getCurrentRawStream(at)
+    except AttributeError:
+        return torch.cuda.current_device(), int(torch.cuda.current_stream().cuda_stream)
+
+
+def _one_device(at: int, tensors):
+    """The launch goes to the current device: all tensors must live there."""
     for t in tensors:
-        if t is not None and t.device.index != at:
+        if t.get_device() != at:
             raise ValueError("all tensors must live on the current device")
-    if stream is not None and getattr(stream, "device_index", at) != at:
-        raise ValueError("stream must belong to the current device")
 
 
 def _new(shape, dtype, like, stream):
@@ -537,10 +550,14 @@ def _new(shape, dtype, like, stream):
         return torch.empty(shape, dtype=dtype, device=like.device)
 
 
-def _rows_strides(t, name: str):
-    """Token and head stride of a [H, L, d] tensor; those of an axis of length one do not matter."""
-    st, sh = _strides(t, name), t.shape
-    return (sh[2] if sh[1] == 1 else st[1]), (0 if sh[0] == 1 else st[0])
+def _rows(t, name: str):
+    """(shape, token stride, head stride) of a [H, L, d] tensor; the stride of an axis of length one does not matter."""
+    if t.is_cuda and t.dtype is (_torch or _get_torch()).bfloat16:
+        st, sh = t.stride(), t.shape
+        if len(st) == 3 and st[2] == 1:
+            return sh, (st[1] if sh[1] != 1 else sh[2]), (st[0] if sh[0] != 1 else 0)
+    _check_tensor(t, name)
+    raise ValueError(f"{name} must be [H, L, d]")
 
 
 def _check_buffer(t, name: str):
@@ -548,36 +565,38 @@ def _check_buffer(t, name: str):
         raise ValueError(f"{name} must be a contiguous uint8 GPU tensor")
 
 
-def _workspace(workspace, need: int, like, stream):
-    """(pointer, bytes) of the caller's scratch or of a new one, and the tensor, to be held until the call returns."""
+def _workspace(workspace, need, like, stream, at: int):
+    """The caller's scratch, or a new one of need() bytes: a tensor, or None where nothing is needed."""
     if workspace is None:
-        if need == 0:
-            return 0, 0, None
-        workspace = _new(need, (_torch or _get_torch()).uint8, like, stream)
-    else:
-        _one_device(None, workspace)
-        if not workspace.is_contiguous():
-            raise ValueError("workspace must be contiguous")
-    return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
+        n = int(need())
+        return _new(n, (_torch or _get_torch()).uint8, like, stream) if n else None
+    if workspace.get_device() != at or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous tensor on the current device")
+    return workspace
 
 
-def _axes_shape(X, g, pos, freq, pairs, heads, d, eps, across_heads, pairing, xs, yst, ysh) -> lf_axes_shape:
+def _bytes_of(t):
+    return (0, 0) if t is None else (t.data_ptr(), t.numel() * t.element_size())
+
+
+def _axes_shape(X, g, pos, freq, pairs, heads, rows, eps, across_heads, pairing) -> lf_axes_shape:
     torch = _torch or _get_torch()
-    for t, dt, name in ((g, torch.float32, "g must be float32 [H * d]"), (pos, torch.int32, "pos must be int32 [L, 3]"),
-                        (freq, torch.float64, "freq must be float64 [d / 2]")):
-        if t.dtype != dt or not t.is_cuda or not t.is_contiguous():
-            raise ValueError(name + ", a contiguous GPU tensor")
-    if X.shape[1] < heads * d or g.numel() != heads * d or pos.shape != (X.shape[0], 3) or freq.numel() != d // 2:
-        raise ValueError("shapes of X, g, pos or freq do not fit")
-    if len(pairs) != 3:
-        raise ValueError("pairs holds the channel pairs of three axes")
-    return lf_axes_shape(heads, d, X.shape[0], int(bool(across_heads)), int(pairing), (C.c_int32 * 3)(*pairs), float(eps), 0,
-                         heads * d if X.shape[0] == 1 else xs, yst, ysh)
-
-
-def _check_rows(t, name: str, dims: int):
-    if t.dtype != (_torch or _get_torch()).bfloat16 or not t.is_cuda or t.dim() != dims or t.stride(-1) != 1:
-        raise ValueError(f"{name} must be a bfloat16 GPU tensor of {dims} axes with contiguous channels")
+    if not X.is_cuda or X.dtype is not torch.bfloat16:
+        raise ValueError("X must be a bfloat16 GPU tensor")
+    if g.dtype is not torch.float32 or not g.is_contiguous():
+        raise ValueError("g must be contiguous float32 [H * d]")
+    if pos.dtype is not torch.int32 or not pos.is_contiguous():
+        raise ValueError("pos must be contiguous int32 [L, 3]")
+    if freq.dtype is not torch.float64 or not freq.is_contiguous():
+        raise ValueError("freq must be contiguous float64 [d / 2]")
+    (yheads, tokens, d), yt, yh = rows
+    xs, xsh = X.stride(), X.shape
+    if len(xs) != 2 or xs[1] != 1 or xsh[0] != tokens or yheads != heads:
+        raise ValueError("X must be [L, >= H * d] with contiguous channels, Y and dY [H, L, d]")
+    if xsh[1] < heads * d or g.numel() != heads * d or pos.shape != (tokens, 3) or freq.numel() != d // 2 or len(pairs) != 3:
+        raise ValueError("shapes of X, g, pos, freq or pairs do not fit")
+    return lf_axes_shape(heads, d, tokens, 1 if across_heads else 0, pairing, tuple(pairs), eps, 0,
+                         xs[0] if tokens != 1 else heads * d, yt, yh)
 
 
 def lf_qk_norm_rope_axes(X, g, pos, freq, pairs, heads: int, Y, eps: float = 1e-6, across_heads: bool = False,
@@ -585,15 +604,11 @@ def lf_qk_norm_rope_axes(X, g, pos, freq, pairs, heads: int, Y, eps: float = 1e-
     """RMSNorm and rotary positions over three axes of the token-major activation X [L, >= H*d] (bfloat16) into the head-major
     tensor Y [H, L, d] (bfloat16; may be a view into Q or into the K cache).  ``pos`` int32 [L, 3] (time, height, width),
     ``freq`` float64 [d/2] in radians per position, ``pairs`` how many channel pairs each axis has."""
-    _check_rows(X, "X", 2)
-    yt, yh = _rows_strides(Y, "Y")
-    heads, (yheads, tokens, d) = int(heads), Y.shape
-    if yheads != heads or tokens != X.shape[0]:
-        raise ValueError("Y must be [H, L, d]")
-    p = _axes_shape(X, g, pos, freq, pairs, heads, d, eps, across_heads, pairing, X.stride(0), yt, yh)
-    _one_device(stream, X, g, pos, freq, Y)
+    p = _axes_shape(X, g, pos, freq, pairs, heads, _rows(Y, "Y"), eps, across_heads, pairing)
+    at, st = _here(stream)
+    _one_device(at, (X, g, pos, freq, Y))
     rc = (_lib or load()).lf_qk_norm_rope_axes(X.data_ptr(), g.data_ptr(), pos.data_ptr(), freq.data_ptr(), C.byref(p),
-                                               Y.data_ptr(), _stream_ptr(stream))
+                                               Y.data_ptr(), st)
     if rc != LF_OK:
         raise LfError(rc, "lf_qk_norm_rope_axes")
     return Y
@@ -611,31 +626,25 @@ def lf_qk_norm_rope_axes_bwd(X, g, pos, freq, pairs, heads: int, dY, eps: float 
     shape and row stride of X, of which the first H*d channels are written, dg float32 [H*d] (``grads``: two such tensors to
     write into instead of new ones)."""
     torch = _torch or _get_torch()
-    _check_rows(X, "X", 2)
-    yt, yh = _rows_strides(dY, "dY")
-    heads, (yheads, tokens, d) = int(heads), dY.shape
-    if yheads != heads or tokens != X.shape[0]:
-        raise ValueError("dY must be [H, L, d]")
-    p = _axes_shape(X, g, pos, freq, pairs, heads, d, eps, across_heads, pairing, X.stride(0), yt, yh)
+    p = _axes_shape(X, g, pos, freq, pairs, heads, _rows(dY, "dY"), eps, across_heads, pairing)
+    at, st = _here(stream)
+    _one_device(at, (X, g, pos, freq, dY))
     if grads is None:
-        dg = _new((heads * d,), torch.float32, X, stream)
-        if tokens == 1 or X.stride(0) == X.shape[1]:
-            dX = _new(tuple(X.shape), torch.bfloat16, X, stream)
-        else:
-            dX = _new((tokens * X.stride(0),), torch.bfloat16, X, stream).as_strided(X.shape, X.stride())
+        tokens, row = p.tokens, X.stride(0)
+        dg = _new(g.shape, torch.float32, X, stream)
+        dX = _new(X.shape, torch.bfloat16, X, stream) if tokens == 1 or row == X.shape[1] else \
+            _new(tokens * row, torch.bfloat16, X, stream).as_strided(X.shape, X.stride())
     else:
         dX, dg = grads
-        _check_rows(dX, "dX", 2)
-        if dX.shape != X.shape or (tokens > 1 and dX.stride(0) != X.stride(0)):
-            raise ValueError("dX must have the shape and strides of X")
-        if dg.dtype != torch.float32 or not dg.is_contiguous() or dg.numel() != heads * d:
-            raise ValueError("dg must be a contiguous float32 GPU tensor [H * d]")
-    _one_device(stream, X, g, pos, freq, dY, dX, dg)
+        if dX.dtype is not torch.bfloat16 or dX.shape != X.shape or dX.stride(1) != 1 or (dX.shape[0] != 1 and dX.stride(0) != X.stride(0)):
+            raise ValueError("dX must be bfloat16 with the shape and strides of X")
+        if dg.dtype is not torch.float32 or not dg.is_contiguous() or dg.numel() != g.numel():
+            raise ValueError("dg must be contiguous float32 [H * d]")
+        _one_device(at, grads)
     lib = _lib or load()
-    ws, nbytes, _keep = _workspace(workspace, 0 if workspace is not None else
-                                   int(lib.lf_qk_norm_rope_axes_bwd_workspace_bytes(C.byref(p))), X, stream)
+    ws = _workspace(workspace, lambda: lib.lf_qk_norm_rope_axes_bwd_workspace_bytes(C.byref(p)), X, stream, at)
     rc = lib.lf_qk_norm_rope_axes_bwd(X.data_ptr(), g.data_ptr(), pos.data_ptr(), freq.data_ptr(), C.byref(p), dY.data_ptr(),
-                                      dX.data_ptr(), dg.data_ptr(), ws, nbytes, _stream_ptr(stream))
+                                      dX.data_ptr(), dg.data_ptr(), *_bytes_of(ws), st)
     if rc != LF_OK:
         raise LfError(rc, "lf_qk_norm_rope_axes_bwd")
     return dX, dg
@@ -649,15 +658,14 @@ def lf_kvq_bytes(heads: int, head_dim: int, capacity: int) -> int:
 def lf_kvq_append(K, V, cache, capacity: int, first: int, stream=None):
     """Write the tokens [first, first + L) of the 4-bit cache from K and V [H, L, d] (bfloat16); returns ``cache`` (a uint8
     device tensor of >= lf_kvq_bytes())."""
-    (kt, kh), (vt, vh) = _rows_strides(K, "K"), _rows_strides(V, "V")
+    (sh, kt, kh), (vsh, vt, vh) = _rows(K, "K"), _rows(V, "V")
     _check_buffer(cache, "cache")
-    if K.shape != V.shape:
+    if sh != vsh:
         raise ValueError("K and V must have one shape")
-    heads, tokens, d = K.shape
-    _one_device(stream, K, V, cache)
-    rc = (_lib or load()).lf_kvq_append(K.data_ptr(), V.data_ptr(), C.byref(lf_kvq_shape(heads, d, int(capacity), 0)),
-                                        C.byref(lf_kvq_rows(int(first), tokens, kt, kh, vt, vh)), cache.data_ptr(), cache.numel(),
-                                        _stream_ptr(stream))
+    at, st = _here(stream)
+    _one_device(at, (K, V, cache))
+    rc = (_lib or load()).lf_kvq_append(K.data_ptr(), V.data_ptr(), C.byref(lf_kvq_shape(sh[0], sh[2], capacity)),
+                                        C.byref(lf_kvq_rows(first, sh[1], kt, kh, vt, vh)), cache.data_ptr(), cache.numel(), st)
     if rc != LF_OK:
         raise LfError(rc, "lf_kvq_append")
     return cache
@@ -667,18 +675,18 @@ def lf_kvq_read(cache, heads: int, head_dim: int, capacity: int, first: int, tok
     """The values that tokens [first, first + tokens) of the 4-bit cache stand for: (K, V), bfloat16 [H, tokens, d]."""
     torch = _torch or _get_torch()
     _check_buffer(cache, "cache")
-    shape = (int(heads), int(tokens), int(head_dim))
+    shape = (heads, tokens, head_dim)
     if K is None:
         K = _new(shape, torch.bfloat16, cache, stream)
     if V is None:
         V = _new(shape, torch.bfloat16, cache, stream)
-    (kt, kh), (vt, vh) = _rows_strides(K, "K"), _rows_strides(V, "V")
-    if tuple(K.shape) != shape or tuple(V.shape) != shape:
+    (ksh, kt, kh), (vsh, vt, vh) = _rows(K, "K"), _rows(V, "V")
+    if ksh != shape or vsh != shape:
         raise ValueError("K and V must be [H, tokens, d]")
-    _one_device(stream, cache, K, V)
-    rc = (_lib or load()).lf_kvq_read(cache.data_ptr(), cache.numel(), C.byref(lf_kvq_shape(shape[0], shape[2], int(capacity), 0)),
-                                      C.byref(lf_kvq_rows(int(first), shape[1], kt, kh, vt, vh)), K.data_ptr(), V.data_ptr(),
-                                      _stream_ptr(stream))
+    at, st = _here(stream)
+    _one_device(at, (cache, K, V))
+    rc = (_lib or load()).lf_kvq_read(cache.data_ptr(), cache.numel(), C.byref(lf_kvq_shape(heads, head_dim, capacity)),
+                                      C.byref(lf_kvq_rows(first, tokens, kt, kh, vt, vh)), K.data_ptr(), V.data_ptr(), st)
     if rc != LF_OK:
         raise LfError(rc, "lf_kvq_read")
     return K, V
@@ -695,32 +703,33 @@ def lf_sparse_attn_kvq(Q, cache, capacity: int, kv_len: int, indices, frame_len:
                        softmax_scale: float = 0.0, O=None, workspace=None, stream=None):
     """Blockwise sparse attention over the 4-bit cache; returns O (bfloat16 [H, q_len, d], device).  With ``K`` and ``V`` [H, q_len,
     d] the current chunk's tokens, the last q_len of kv_len, are read from them in bfloat16, without them from the cache."""
-    torch = _torch or _get_torch()
-    if (K is None) != (V is None):
-        raise ValueError("K and V go together")
     _check_buffer(cache, "cache")
-    qt, qh = _rows_strides(Q, "Q")
-    heads, q_len, d = Q.shape
-    kt = kh = vt = vh = 0
-    if K is not None:
-        (kt, kh), (vt, vh) = _rows_strides(K, "K"), _rows_strides(V, "V")
-        if K.shape != Q.shape or V.shape != Q.shape:
-            raise ValueError("K and V must be [H, q_len, d], the current chunk's tokens")
+    qsh, qt, qh = _rows(Q, "Q")
+    heads, q_len, d = qsh
     if O is None:
-        O = _new((heads, q_len, d), torch.bfloat16, Q, stream)
-    ot, oh = _rows_strides(O, "O")
-    if O.shape != Q.shape:
+        O = _new(qsh, (_torch or _get_torch()).bfloat16, Q, stream)
+    osh, ot, oh = _rows(O, "O")
+    if osh != qsh:
         raise ValueError("O must be [H, q_len, d]")
-    sh = lf_shape(heads, d, int(frame_len), int(block), q_len, int(kv_len), LF_BF16, 0, qt, qh, kt, kh, vt, vh, ot, oh)
+    at, st = _here(stream)
+    kt = kh = vt = vh = k_ptr = v_ptr = 0
+    if K is not None and V is not None:
+        (ksh, kt, kh), (vsh, vt, vh) = _rows(K, "K"), _rows(V, "V")
+        if ksh != qsh or vsh != qsh:
+            raise ValueError("K and V must be [H, q_len, d], the current chunk's tokens")
+        _one_device(at, (Q, cache, indices, K, V, O))
+        k_ptr, v_ptr = K.data_ptr(), V.data_ptr()
+    elif K is not None or V is not None:
+        raise ValueError("K and V go together")
+    else:
+        _one_device(at, (Q, cache, indices, O))
+    sh = lf_shape(heads, d, frame_len, block, q_len, kv_len, LF_BF16, 0, qt, qh, kt, kh, vt, vh, ot, oh)
     _check_lists(indices, sh, frame_len)
-    _one_device(stream, Q, cache, indices, K, V, O)
+    length = indices.shape[2]
     lib = _lib or load()
-    ws, nbytes, _keep = _workspace(workspace, 0 if workspace is not None else
-                                   int(lib.lf_sparse_attn_kvq_workspace_bytes(C.byref(sh), indices.shape[2])), Q, stream)
-    rc = lib.lf_sparse_attn_kvq(Q.data_ptr(), cache.data_ptr(), cache.numel(), C.byref(lf_kvq_shape(heads, d, int(capacity), 0)),
-                                None if K is None else K.data_ptr(), None if V is None else V.data_ptr(), C.byref(sh),
-                                indices.data_ptr(), indices.shape[2], float(softmax_scale), O.data_ptr(), ws, nbytes,
-                                _stream_ptr(stream))
+    ws = _workspace(workspace, lambda: lib.lf_sparse_attn_kvq_workspace_bytes(C.byref(sh), length), Q, stream, at)
+    rc = lib.lf_sparse_attn_kvq(Q.data_ptr(), cache.data_ptr(), cache.numel(), C.byref(lf_kvq_shape(heads, d, capacity)),
+                                k_ptr, v_ptr, C.byref(sh), indices.data_ptr(), length, softmax_scale, O.data_ptr(), *_bytes_of(ws), st)
     if rc != LF_OK:
         raise LfError(rc, "lf_sparse_attn_kvq")
     return O
@@ -736,31 +745,32 @@ def lf_token_attn_kvq(Q, cache, capacity: int, cached_len: int, K=None, V=None, 
                       workspace=None, stream=None):
     """Attention of up to 64 query rows [H, q_len, d] over the first ``cached_len`` tokens of the 4-bit cache and the tokens of ``K``
     and ``V`` [H, extra, d] (bfloat16, optional) behind them; returns O (bfloat16 [H, q_len, d], device)."""
-    torch = _torch or _get_torch()
-    if (K is None) != (V is None):
-        raise ValueError("K and V go together")
     _check_buffer(cache, "cache")
-    qt, qh = _rows_strides(Q, "Q")
-    heads, q_len, d = Q.shape
-    extra = kt = kh = vt = vh = 0
-    if K is not None:
-        (kt, kh), (vt, vh) = _rows_strides(K, "K"), _rows_strides(V, "V")
-        extra = K.shape[1]
-        if K.shape != V.shape or K.shape[0] != heads or K.shape[2] != d:
-            raise ValueError("K and V must be [H, extra, d]")
+    qsh, qt, qh = _rows(Q, "Q")
+    heads, q_len, d = qsh
     if O is None:
-        O = _new((heads, q_len, d), torch.bfloat16, Q, stream)
-    ot, oh = _rows_strides(O, "O")
-    if O.shape != Q.shape:
+        O = _new(qsh, (_torch or _get_torch()).bfloat16, Q, stream)
+    osh, ot, oh = _rows(O, "O")
+    if osh != qsh:
         raise ValueError("O must be [H, q_len, d]")
-    sh = lf_token_shape(heads, d, q_len, int(cached_len), extra, 0, qt, qh, kt, kh, vt, vh, ot, oh)
-    _one_device(stream, Q, cache, K, V, O)
+    at, st = _here(stream)
+    extra = kt = kh = vt = vh = k_ptr = v_ptr = 0
+    if K is not None and V is not None:
+        (ksh, kt, kh), (vsh, vt, vh) = _rows(K, "K"), _rows(V, "V")
+        extra = ksh[1]
+        if ksh != vsh or ksh[0] != heads or ksh[2] != d:
+            raise ValueError("K and V must be [H, extra, d]")
+        _one_device(at, (Q, cache, K, V, O))
+        k_ptr, v_ptr = K.data_ptr(), V.data_ptr()
+    elif K is not None or V is not None:
+        raise ValueError("K and V go together")
+    else:
+        _one_device(at, (Q, cache, O))
+    sh = lf_token_shape(heads, d, q_len, cached_len, extra, 0, qt, qh, kt, kh, vt, vh, ot, oh)
     lib = _lib or load()
-    ws, nbytes, _keep = _workspace(workspace, 0 if workspace is not None else
-                                   int(lib.lf_token_attn_kvq_workspace_bytes(C.byref(sh))), Q, stream)
-    rc = lib.lf_token_attn_kvq(Q.data_ptr(), cache.data_ptr(), cache.numel(), C.byref(lf_kvq_shape(heads, d, int(capacity), 0)),
-                               None if K is None else K.data_ptr(), None if V is None else V.data_ptr(), C.byref(sh),
-                               float(softmax_scale), O.data_ptr(), ws, nbytes, _stream_ptr(stream))
+    ws = _workspace(workspace, lambda: lib.lf_token_attn_kvq_workspace_bytes(C.byref(sh)), Q, stream, at)
+    rc = lib.lf_token_attn_kvq(Q.data_ptr(), cache.data_ptr(), cache.numel(), C.byref(lf_kvq_shape(heads, d, capacity)),
+                               k_ptr, v_ptr, C.byref(sh), softmax_scale, O.data_ptr(), *_bytes_of(ws), st)
     if rc != LF_OK:
         raise LfError(rc, "lf_token_attn_kvq")
     return O
