@@ -97,6 +97,9 @@ int check_lists(const lf_shape* s, int32_t list_len, lf_dims* dm) {
   return list_len < 1 ? LF_ERR_BUDGET : LF_OK;
 }
 
+// K or V of all tokens in bfloat16, padded to 256 bytes.
+size_t expanded_bytes(const lf_dims& dm) { return ((size_t)dm.H * dm.F * dm.n * dm.d * 2 + 255) / 256 * 256; }
+
 int list_rows(const lf_dims& dm) { return dm.n < 64 ? dm.n : 64; }
 
 }  // namespace
@@ -159,6 +162,7 @@ extern "C" size_t lf_sparse_attn_kvq_workspace_bytes(const lf_shape* s, int32_t 
   lf_dims dm;
   if (check_lists(s, list_len, &dm) != LF_OK) return 0;
   const int64_t blocks = (int64_t)dm.H * dm.n_q;
+  if (lf_kvq_expands(dm.d, blocks, list_len, dm.H, s->kv_len)) return 2 * expanded_bytes(dm);
   return (size_t)lf_kvq_state_bytes(blocks, lf_kvq_parts_of(blocks, list_len), list_rows(dm), dm.d);
 }
 
@@ -197,7 +201,16 @@ extern "C" int lf_sparse_attn_kvq(const void* Q, const void* cache, size_t cache
   c.cached = cached;
   c.extra = s->kv_len - cached;
   c.rows = list_rows(dm);
-  c.parts = lf_kvq_parts_of((int64_t)dm.H * dm.n_q, list_len);
+  const int64_t blocks = (int64_t)dm.H * dm.n_q;
+  if (lf_kvq_expands(dm.d, blocks, list_len, dm.H, s->kv_len)) {
+    uint16_t *Kw = (uint16_t*)workspace, *Vw = (uint16_t*)((char*)workspace + expanded_bytes(dm));
+    if ((rc = lf_launch_kvq_expand(&c, Kw, Vw, stream)) != LF_OK) return rc;
+    lf_shape t = *s;
+    t.k_stride_tok = t.v_stride_tok = dm.d;
+    t.k_stride_head = t.v_stride_head = (int64_t)s->kv_len * dm.d;
+    return lf_launch_attn(Q, Kw, Vw, &t, &dm, indices, list_len, list_len, c.scale, O, nullptr, nullptr, nullptr, stream);
+  }
+  c.parts = lf_kvq_parts_of(blocks, list_len);
   c.workspace = workspace;
   return lf_launch_kvq_attn(&c, stream);
 }

@@ -13,11 +13,14 @@
 // so P stays in its registers; V goes through LDS as bfloat16 rows and comes back by the transposing read.  The bytes of
 // the next tile are requested as soon as those of the present one are converted.
 //
-// Softmax is float32 in the exp2 domain, P = exp2(s c - m), against a reference m per row that moves only when a score passes it by
-// more than 8: without that no lane asks another.  P is rounded to bfloat16 for the product (as the output is), sums of it are float32.
+// Softmax is float32 in the exp2 domain, P = exp2(s c - m), against a reference m per row that moves only when a P passes 2^8: without
+// that no lane asks another and no maximum of scores is taken.  P is rounded to bfloat16 for the product (as the output is); the row's sum
+// is the product of the same P with ones, in float32.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
+
+#include <type_traits>
 
 #include "lf_rollout.h"
 
@@ -27,6 +30,7 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 struct KvqAttnArgs {
   const uint16_t *Q, *Kx, *Vx;
@@ -43,13 +47,12 @@ struct KvqAttnArgs {
 };
 
 constexpr int kWaves = 4;
-constexpr float kSlack = 8.0f;      // how far a score may pass the reference: P stays below 2^8
+constexpr float kMostP = 256.0f;    // a larger P moves the reference
 
 #define LDS_PTR(T, p) ((__attribute__((address_space(3))) T*)(p))
 
 union Frag {
-  uint4 u;
-  uint32_t w[4];
+  u32x4 x;
   bf16x2 p[4];
   bf16x8 v;
 };
@@ -65,22 +68,23 @@ __device__ __forceinline__ Frag decode(uint32_t code, float scale) {
 }
 __device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }   // 255: the conversion gives NaN
 
-// Up to 32 tokens side by side, in the cache or behind it; cnt = 0: none.
+// Up to 64 tokens side by side; cnt = 0: none.
 struct Tile {
   int tok, cnt;
-  bool ext;
 };
 
-template <int D, int NQ, bool LISTS>
-__global__ __launch_bounds__(64 * kWaves, NQ == 4 && D == 128 ? 1 : 2) void lf_kvq_attn_kernel(KvqAttnArgs a) {
+template <int D, int NQ, int RG, bool LISTS>
+__global__ __launch_bounds__(64 * kWaves, 2) void lf_kvq_attn_kernel(KvqAttnArgs a) {
   constexpr int KS = D / 32;          // steps of the first product, 8 channels of a lane each
   constexpr int MB = D / 16;          // tiles of 16 channels of the second
   constexpr int CW = D / 32;          // words of codes of a lane and token (D / 4 channels)
   constexpr int CH = D / 8;           // 16-byte chunks of a row in LDS
-  constexpr int VI = D / 64;          // scaled groups of V's tile for a lane
-  __shared__ uint4 stage[kWaves][32 * CH];
+  constexpr int VI = D / 64;          // scaled groups of half a tile's V for a lane
+  constexpr int SL = kWaves / RG;     // tiles at a time
+  __shared__ u32x4 stage[kWaves][32 * CH];
   __shared__ float2 ml[kWaves][16 * NQ];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int rg = wave % RG, slot = wave / RG;
   const int col = lane & 15, kg = lane >> 4;
   const int part = blockIdx.x % a.parts, blk = blockIdx.x / a.parts;      // blk: (head, query block)
   const int h = LISTS ? blk / a.n_q : blk, r = LISTS ? blk % a.n_q : 0;
@@ -100,51 +104,46 @@ __global__ __launch_bounds__(64 * kWaves, NQ == 4 && D == 128 ? 1 : 2) void lf_k
   Frag qf[NQ][KS];
 #pragma unroll
   for (int q = 0; q < NQ; ++q) {
-    const int row = row0 + min(16 * q + col, rows - 1);
+    const int row = row0 + min(16 * (NQ * rg + q) + col, rows - 1);
     const uint16_t* p = a.Q + (int64_t)h * a.q_stride_head + (int64_t)row * a.q_stride_tok + (D / 4) * kg;
 #pragma unroll
-    for (int u = 0; u < KS; ++u) qf[q][u].u = *reinterpret_cast<const uint4*>(p + 8 * u);
+    for (int u = 0; u < KS; ++u) qf[q][u].x = *reinterpret_cast<const u32x4*>(p + 8 * u);
   }
 
-  // The tiles of this wavefront, in turn: entry `at` of the list (or block of 64 tokens), then its second half.
-  const int units = LISTS ? a.list_len : (a.cached + 63) / 64 + (a.extra + 63) / 64;
-  int at = part * kWaves + wave, half = 0;
-  auto next = [&]() __attribute__((always_inline)) {
-    Tile t = {0, 0, false};
-    while (at < units) {
-      int tok, cnt;
-      bool ext;
+  // The tiles of this wavefront, in turn: every (parts SL)-th entry of the list, or block of 64 tokens; those in the cache (EXT = false), then
+  // those behind it.
+  const int held = (a.cached + 63) / 64;
+  const int units = LISTS ? a.list_len : held + (a.extra + 63) / 64;
+  const int stride = a.parts * SL;
+  int at, ahead;                // the next entry, and for lists what it says
+  auto begin = [&]() __attribute__((always_inline)) {
+    at = part * SL + slot;
+    ahead = LISTS && at < units ? list[at] : 0;
+  };
+  auto next = [&](bool ext) __attribute__((always_inline)) {
+    Tile t = {0, 0};
+    while (at < units && t.cnt == 0) {
       if constexpr (LISTS) {
-        const int id = __builtin_amdgcn_readfirstlane(list[at]);
-        ext = id >= a.nb_cached;
+        const int id = __builtin_amdgcn_readfirstlane(ahead);
+        if (at + stride < units) ahead = list[at + stride];
         const int frame = id / a.nb, j = id - frame * a.nb;
-        tok = (ext ? frame - a.nb_cached / a.nb : frame) * a.n + 64 * j;
-        cnt = id >= 0 && id < a.n_k ? min(64, a.n - 64 * j) : 0;
-      } else {
-        const int held = (a.cached + 63) / 64;
-        ext = at >= held;
-        tok = 64 * (ext ? at - held : at);
-        cnt = min(64, (ext ? a.extra : a.cached) - tok);
+        t.tok = (ext ? frame - a.nb_cached / a.nb : frame) * a.n + 64 * j;
+        t.cnt = id >= (ext ? a.nb_cached : 0) && id < (ext ? a.n_k : a.nb_cached) ? min(64, a.n - 64 * j) : 0;
+      } else if ((at >= held) == ext) {
+        t.tok = 64 * (ext ? at - held : at);
+        t.cnt = min(64, (ext ? a.extra : a.cached) - t.tok);
       }
-      if (cnt > 32 * half) {
-        t.tok = tok + 32 * half;
-        t.cnt = min(32, cnt - 32 * half);
-        t.ext = ext;
-        if (cnt > 32 && half == 0) half = 1;
-        else { half = 0; at += a.parts * kWaves; }
-        return t;
-      }
-      half = 0;
-      at += a.parts * kWaves;
+      at += stride;
     }
     return t;
   };
 
-  uint32_t kw[2][CW], vw[VI][4], ksc[2], vsc[VI];
-  auto load = [&](const Tile& t) __attribute__((always_inline)) {
-    if (t.cnt == 0 || t.ext) return;
+  // The bytes of a tile: a lane's D/4 channels of four tokens of K, and its groups of V, half a tile at a time.
+  uint32_t kw[4][CW], ksc[4], vw[2][VI][4], vsc[2][VI];
+  auto load_k = [&](const Tile& t) __attribute__((always_inline)) {
+    if (t.cnt == 0) return;
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
+    for (int s = 0; s < 4; ++s) {
       const int row = t.tok + min(16 * s + col, t.cnt - 1);
       const uint8_t* p = kc + (uint32_t)row * (D / 2) + (D / 8) * kg;
       if constexpr (CW == 4) {
@@ -156,134 +155,189 @@ __global__ __launch_bounds__(64 * kWaves, NQ == 4 && D == 128 ? 1 : 2) void lf_k
       }
       ksc[s] = ks[(uint32_t)row * (D / 32) + (D == 128 ? kg : kg >> 1)];
     }
+  };
+  auto load_v = [&](const Tile& t, int half) __attribute__((always_inline)) {
+    if (t.cnt == 0) return;
 #pragma unroll
     for (int i = 0; i < VI; ++i) {
-      const int item = 64 * i + lane, row = t.tok + min(item / (D / 32), t.cnt - 1), grp = item % (D / 32);
+      const int item = 64 * i + lane, row = t.tok + min(32 * half + item / (D / 32), t.cnt - 1), grp = item % (D / 32);
       const uint4 x = *reinterpret_cast<const uint4*>(vc + (uint32_t)row * (D / 2) + 16 * grp);
-      vw[i][0] = x.x; vw[i][1] = x.y; vw[i][2] = x.z; vw[i][3] = x.w;
-      vsc[i] = vs[(uint32_t)row * (D / 32) + grp];
+      vw[half][i][0] = x.x; vw[half][i][1] = x.y; vw[half][i][2] = x.z; vw[half][i][3] = x.w;
+      vsc[half][i] = vs[(uint32_t)row * (D / 32) + grp];
     }
   };
 
   f32x4 oacc[NQ][MB];
-  float m_run[NQ], l_run[NQ];
+  f32x4 lacc[NQ];               // row sums: the product of P with ones, the same in every row of the result
+  float m_run[NQ];
+  bool first = true;
 #pragma unroll
   for (int q = 0; q < NQ; ++q) {
     m_run[q] = -INFINITY;
-    l_run[q] = 0.0f;
+    lacc[q] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int mb = 0; mb < MB; ++mb) oacc[q][mb] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   }
+  bf16x8 ones;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) ones[i] = (__bf16)1.0f;
   // Rows of V in LDS: the transposing read takes 32 bytes of four rows at a time, which land in different banks when the row's two low bits
   // go to the chunk's high bits (d = 128) or its second bit does (d = 64).
   auto swz = [](int row, int ch) __attribute__((always_inline)) { return CH == 16 ? ch ^ ((row & 3) << 2) : ch ^ (((row >> 1) & 1) << 2); };
-  uint4* vt = stage[wave];
+  u32x4* vt = stage[wave];
+  // A lane writes the four chunks of its group in an order of its own: in one order all lanes would write the same quarter of the banks at a time.
+  const int rot = lane >> 2 & 3;
+  const bool rot1 = lane & 4, rot2 = lane & 8;
+  auto own_lds = []() __attribute__((always_inline)) {    // this wavefront's own rows: LDS keeps its order, and the compiler its own
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+  };
 
-  Tile cur = next();
-  load(cur);
-  while (cur.cnt > 0) {
-    Frag kf[2][KS];
-    if (!cur.ext) {
-#pragma unroll
-      for (int s = 0; s < 2; ++s)
-#pragma unroll
-        for (int u = 0; u < KS; ++u) kf[s][u] = decode(kw[s][u], scale_of(ksc[s]));
+  auto tile = [&](auto ext_c, const Tile& cur, const Tile& then) __attribute__((always_inline)) {
+    constexpr bool EXT = decltype(ext_c)::value;
+    auto stage_v = [&](int half) __attribute__((always_inline)) {
+      own_lds();
 #pragma unroll
       for (int i = 0; i < VI; ++i) {
         const int item = 64 * i + lane, row = item / (D / 32), grp = item % (D / 32);
+        u32x4 y[4];
+        if constexpr (!EXT) {
+          uint32_t x[4], z[4];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) vt[row * CH + swz(row, 4 * grp + u)] = decode(vw[i][u], scale_of(vsc[i])).u;
+          for (int u = 0; u < 4; ++u) x[u] = rot1 ? vw[half][i][(u + 1) & 3] : vw[half][i][u];
+#pragma unroll
+          for (int u = 0; u < 4; ++u) z[u] = rot2 ? x[(u + 2) & 3] : x[u];
+#pragma unroll
+          for (int u = 0; u < 4; ++u) y[u] = decode(z[u], scale_of(vsc[half][i])).x;
+        } else {
+          const int tok = cur.tok + min(32 * half + row, cur.cnt - 1);
+          const uint16_t* p = a.Vx + (int64_t)h * a.v_stride_head + (int64_t)tok * a.v_stride_tok + 32 * grp;
+#pragma unroll
+          for (int u = 0; u < 4; ++u) y[u] = *reinterpret_cast<const u32x4*>(p + 8 * ((u + rot) & 3));
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) vt[row * CH + swz(row, 4 * grp + ((u + rot) & 3))] = y[u];
       }
-    } else {
+      own_lds();
+      if constexpr (!EXT) load_v(then, half);
+    };
+    f32x4 sacc[NQ][4];
 #pragma unroll
-      for (int s = 0; s < 2; ++s) {
+    for (int s = 0; s < 4; ++s) {
+      Frag kf[KS];
+      if constexpr (!EXT) {
+#pragma unroll
+        for (int u = 0; u < KS; ++u) kf[u] = decode(kw[s][u], scale_of(ksc[s]));
+      } else {
         const int row = cur.tok + min(16 * s + col, cur.cnt - 1);
         const uint16_t* p = a.Kx + (int64_t)h * a.k_stride_head + (int64_t)row * a.k_stride_tok + (D / 4) * kg;
 #pragma unroll
-        for (int u = 0; u < KS; ++u) kf[s][u].u = *reinterpret_cast<const uint4*>(p + 8 * u);
+        for (int u = 0; u < KS; ++u) kf[u].x = *reinterpret_cast<const u32x4*>(p + 8 * u);
       }
 #pragma unroll
-      for (int i = 0; i < VI; ++i) {
-        const int item = 64 * i + lane, row = item / (D / 32), grp = item % (D / 32);
-        const uint16_t* p = a.Vx + (int64_t)h * a.v_stride_head + (int64_t)(cur.tok + min(row, cur.cnt - 1)) * a.v_stride_tok + 32 * grp;
-#pragma unroll
-        for (int u = 0; u < 4; ++u) vt[row * CH + swz(row, 4 * grp + u)] = *reinterpret_cast<const uint4*>(p + 8 * u);
-      }
-    }
-    const Tile then = next();
-    load(then);
-
-    f32x4 sacc[NQ][2];
-#pragma unroll
-    for (int q = 0; q < NQ; ++q)
-#pragma unroll
-      for (int s = 0; s < 2; ++s) {
+      for (int q = 0; q < NQ; ++q) {
         sacc[q][s] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int u = 0; u < KS; ++u) sacc[q][s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[s][u].v, qf[q][u].v, sacc[q][s], 0, 0, 0);
+        for (int u = 0; u < KS; ++u) sacc[q][s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[u].v, qf[q][u].v, sacc[q][s], 0, 0, 0);
       }
-    bf16x8 pf[NQ];
+    }
+    if constexpr (!EXT) load_k(then);
+    stage_v(0);
+    if (cur.cnt < 64) {       // (the tile's last token stands in for those behind it)
 #pragma unroll
-    for (int q = 0; q < NQ; ++q) {
-      float s[8];
+      for (int q = 0; q < NQ; ++q)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) s[i] = sacc[q][i >> 2][i & 3] * a.c;
-      if (cur.cnt < 32) {       // (the tile's last tokens are there twice)
+        for (int s = 0; s < 4; ++s)
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (16 * (i >> 2) + 4 * kg + (i & 3) >= cur.cnt) s[i] = -INFINITY;
-      }
-      float top = s[0];
+          for (int i = 0; i < 4; ++i)
+            if (16 * s + 4 * kg + i >= cur.cnt) sacc[q][s][i] = -INFINITY;
+    }
+    // P against the reference as it stands; where that is too low (or not set yet: the wavefront's first tile) it moves up to the maxima and P
+    // is made again.
+    float p[NQ][16];
+    auto weights = [&]() __attribute__((always_inline)) {
 #pragma unroll
-      for (int i = 1; i < 8; ++i) top = fmaxf(top, s[i]);
-      if (__ballot(top > m_run[q] + kSlack) != 0ull) {
+      for (int q = 0; q < NQ; ++q)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) p[q][i] = __builtin_amdgcn_exp2f(fmaf(sacc[q][i >> 2][i & 3], a.c, -m_run[q]));
+    };
+    bool move = first;
+    if (!first) {
+      weights();
+      float most = 0.0f;
+#pragma unroll
+      for (int q = 0; q < NQ; ++q)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) most = fmaxf(most, p[q][i]);
+      move = __ballot(most > kMostP) != 0ull;
+    }
+    if (move) {
+#pragma unroll
+      for (int q = 0; q < NQ; ++q) {
+        float top = sacc[q][0][0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) top = fmaxf(top, sacc[q][i >> 2][i & 3]);
         top = fmaxf(top, __shfl_xor(top, 16));
-        top = fmaxf(top, __shfl_xor(top, 32));
-        const float m_new = fmaxf(m_run[q], top);
-        // a row without a finite score yet keeps its sums of zero
-        const float alpha = m_new == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m_run[q] - m_new);
+        top = fmaxf(top, __shfl_xor(top, 32)) * a.c;
+        const float m_new = first ? top : fmaxf(m_run[q], top);
+        const float alpha = first ? 0.0f : __builtin_amdgcn_exp2f(m_run[q] - m_new);
         m_run[q] = m_new;
-        l_run[q] *= alpha;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) lacc[q][i] *= alpha;
 #pragma unroll
         for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
           for (int i = 0; i < 4; ++i) oacc[q][mb][i] *= alpha;
       }
-      const float m = m_run[q] == -INFINITY ? 0.0f : m_run[q];
+      weights();
+      first = false;
+    }
+    bf16x8 pf[NQ][2];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float p = __builtin_amdgcn_exp2f(s[i] - m);
-        l_run[q] += p;
-        pf[q][i] = (__bf16)p;
+    for (int q = 0; q < NQ; ++q)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) pf[q][i >> 3][i & 7] = (__bf16)p[q][i];
+#pragma unroll
+    for (int q = 0; q < NQ; ++q)
+#pragma unroll
+      for (int half = 0; half < 2; ++half) lacc[q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pf[q][half], lacc[q], 0, 0, 0);
+    auto product = [&](int half) __attribute__((always_inline)) {
+      const uint16_t* v16 = reinterpret_cast<const uint16_t*>(vt);
+#pragma unroll
+      for (int mb = 0; mb < MB; ++mb) {
+        const int vrow = 4 * kg + (col >> 2), vcol = 16 * mb + 4 * (col & 3);
+        const int off = (vrow * CH + swz(vrow, vcol >> 3)) * 8 + (vcol & 7);      // (16 rows on the swizzle is the same)
+        const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(LDS_PTR(bf16x4, v16 + off));
+        const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(LDS_PTR(bf16x4, v16 + off + 16 * CH * 8));
+        const bf16x8 vf = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) oacc[q][mb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[q][half], oacc[q][mb], 0, 0, 0);
       }
-    }
-    // this wavefront's own rows: LDS keeps its order, and the compiler its own
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
-    const uint16_t* v16 = reinterpret_cast<const uint16_t*>(vt);
-#pragma unroll
-    for (int mb = 0; mb < MB; ++mb) {
-      const int vrow = 4 * kg + (col >> 2), vcol = 16 * mb + 4 * (col & 3);
-      const int off = (vrow * CH + swz(vrow, vcol >> 3)) * 8 + (vcol & 7);      // (16 rows on the swizzle is the same)
-      const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(LDS_PTR(bf16x4, v16 + off));
-      const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(LDS_PTR(bf16x4, v16 + off + 16 * CH * 8));
-      const bf16x8 vf = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-#pragma unroll
-      for (int q = 0; q < NQ; ++q) oacc[q][mb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[q], oacc[q][mb], 0, 0, 0);
-    }
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+    };
+    product(0);
+    stage_v(1);
+    product(1);
+  };
+  begin();
+  Tile cur = next(false);
+  load_k(cur);
+  load_v(cur, 0);
+  load_v(cur, 1);
+  while (cur.cnt > 0) {
+    const Tile then = next(false);
+    tile(std::false_type{}, cur, then);
     cur = then;
   }
+  if (a.extra > 0) {
+    begin();
+    for (Tile t = next(true); t.cnt > 0; t = next(true)) tile(std::true_type{}, t, t);
+  }
 
-  // The four wavefronts' states become one.
+  // The states of the SL wavefronts that have the same rows become one.
 #pragma unroll
   for (int q = 0; q < NQ; ++q) {
-    l_run[q] += __shfl_xor(l_run[q], 16);
-    l_run[q] += __shfl_xor(l_run[q], 32);
-    if (kg == 0) ml[wave][16 * q + col] = make_float2(m_run[q], l_run[q]);
+    if (kg == 0) ml[wave][16 * q + col] = make_float2(m_run[q], lacc[q][0]);
   }
   __syncthreads();
   f32x4* buf = reinterpret_cast<f32x4*>(&stage[0][0]);        // MB tiles of four wavefronts, 64 lanes each: the whole stage
@@ -291,10 +345,10 @@ __global__ __launch_bounds__(64 * kWaves, NQ == 4 && D == 128 ? 1 : 2) void lf_k
   for (int q = 0; q < NQ; ++q) {
     float M = -INFINITY, L = 0.0f;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) M = fmaxf(M, ml[w][16 * q + col].x);
+    for (int w = 0; w < SL; ++w) M = fmaxf(M, ml[RG * w + rg][16 * q + col].x);
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      const float2 x = ml[w][16 * q + col];
+    for (int w = 0; w < SL; ++w) {
+      const float2 x = ml[RG * w + rg][16 * q + col];
       L += x.x == -INFINITY ? 0.0f : x.y * __builtin_amdgcn_exp2f(x.x - M);
     }
     const float f = m_run[q] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m_run[q] - M);
@@ -306,14 +360,14 @@ __global__ __launch_bounds__(64 * kWaves, NQ == 4 && D == 128 ? 1 : 2) void lf_k
       buf[(mb * kWaves + wave) * 64 + lane] = o;
     }
     __syncthreads();
-    const int row = 16 * q + col;
+    const int row = 16 * (NQ * rg + q) + col;
 #pragma unroll
-    for (int k = 0; k < MB / kWaves; ++k) {
-      const int mb = k * kWaves + wave;
-      f32x4 o = buf[mb * kWaves * 64 + lane];
+    for (int k = 0; k < MB / SL; ++k) {
+      const int mb = k * SL + slot;
+      f32x4 o = buf[(mb * kWaves + rg) * 64 + lane];
 #pragma unroll
-      for (int w = 1; w < kWaves; ++w) {
-        const f32x4 x = buf[(mb * kWaves + w) * 64 + lane];
+      for (int w = 1; w < SL; ++w) {
+        const f32x4 x = buf[(mb * kWaves + RG * w + rg) * 64 + lane];
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[i] += x[i];
       }
@@ -326,22 +380,21 @@ __global__ __launch_bounds__(64 * kWaves, NQ == 4 && D == 128 ? 1 : 2) void lf_k
           *reinterpret_cast<bf16x4*>(a.O + (int64_t)h * a.o_stride_head + (int64_t)(row0 + row) * a.o_stride_tok + 16 * mb + 4 * kg) = y;
         }
       } else {
-        *reinterpret_cast<f32x4*>(a.state_o + (((int64_t)blockIdx.x * 16 * NQ + row) * D + 16 * mb + 4 * kg)) = o;
+        *reinterpret_cast<f32x4*>(a.state_o + (((int64_t)blockIdx.x * 16 * NQ * RG + row) * D + 16 * mb + 4 * kg)) = o;
       }
     }
-    if (a.parts > 1 && wave == 0 && kg == 0) a.state_ml[(int64_t)blockIdx.x * 16 * NQ + row] = make_float2(M, L);
+    if (a.parts > 1 && slot == 0 && kg == 0) a.state_ml[(int64_t)blockIdx.x * 16 * NQ * RG + row] = make_float2(M, L);
     __syncthreads();
   }
 }
 
-// Joins the parts of a row: a wavefront each, lane p holding part p's weight.
+// Joins the parts of a row: a workgroup each, its wavefronts taking every fourth part, lane p holding part p's weight.
 template <int D>
-__global__ __launch_bounds__(256) void lf_kvq_join_kernel(KvqAttnArgs a, int rows_max, int tile_rows, int H) {
+__global__ __launch_bounds__(64 * kWaves) void lf_kvq_join_kernel(KvqAttnArgs a, int rows_max, int tile_rows) {
   constexpr int W = D / 64;       // channels of a lane
-  const int lane = threadIdx.x & 63;
-  const int64_t row = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int blk = (int)(row / rows_max), i = (int)(row % rows_max);
-  if (blk >= H * a.n_q) return;
+  __shared__ float sums[kWaves][D];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int blk = blockIdx.x / rows_max, i = blockIdx.x % rows_max;
   const int h = blk / a.n_q, r = blk % a.n_q;
   int row0 = 0, rows = a.q_len;
   if (a.idx) {
@@ -353,32 +406,48 @@ __global__ __launch_bounds__(256) void lf_kvq_join_kernel(KvqAttnArgs a, int row
   const int64_t first = (int64_t)blk * a.parts * tile_rows + i;      // row of part 0; the others tile_rows apart
   float2 x = make_float2(-INFINITY, 0.0f);
   if (lane < a.parts) x = a.state_ml[first + (int64_t)lane * tile_rows];
+  // a wavefront's parts are requested before the weights are known
+  constexpr int N = LF_KVQ_MAX_PARTS / kWaves;
+  float v[N][W], o[W];
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    const int p = wave + kWaves * k;
+#pragma unroll
+    for (int e = 0; e < W; ++e) v[k][e] = p < a.parts ? a.state_o[(first + (int64_t)p * tile_rows) * D + W * lane + e] : 0.0f;
+  }
   float M = x.x;
 #pragma unroll
   for (int off = 1; off < 64; off <<= 1) M = fmaxf(M, __shfl_xor(M, off));
   const float wgt = x.x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(x.x - M);
+#pragma unroll
+  for (int e = 0; e < W; ++e) o[e] = 0.0f;
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    const float w = __shfl(wgt, wave + kWaves * k);       // 0 behind the last part
+#pragma unroll
+    for (int e = 0; e < W; ++e) o[e] = fmaf(w, v[k][e], o[e]);
+  }
+#pragma unroll
+  for (int e = 0; e < W; ++e) sums[wave][W * lane + e] = o[e];
+  __syncthreads();
+  if (wave != 0) return;
   float L = wgt == 0.0f ? 0.0f : wgt * x.y;
 #pragma unroll
   for (int off = 1; off < 64; off <<= 1) L += __shfl_xor(L, off);
   const float inv = L > 0.0f || L != L ? 1.0f / L : 0.0f;
-  float o[W];
-#pragma unroll
-  for (int e = 0; e < W; ++e) o[e] = 0.0f;
-#pragma unroll 4
-  for (int p = 0; p < a.parts; ++p) {
-    const float w = __shfl(wgt, p);
-    const float* from = a.state_o + (first + (int64_t)p * tile_rows) * D + W * lane;
-#pragma unroll
-    for (int e = 0; e < W; ++e) o[e] = fmaf(w, from[e], o[e]);
-  }
   uint16_t* to = a.O + (int64_t)h * a.o_stride_head + (int64_t)(row0 + i) * a.o_stride_tok + W * lane;
 #pragma unroll
-  for (int e = 0; e < W; ++e) reinterpret_cast<__bf16*>(to)[e] = (__bf16)(o[e] * inv);
+  for (int e = 0; e < W; ++e) {
+    float v = sums[0][W * lane + e];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) v += sums[w][W * lane + e];
+    reinterpret_cast<__bf16*>(to)[e] = (__bf16)(v * inv);
+  }
 }
 
 template <int D, bool LISTS>
 void (*attn_kernel(int tiles))(KvqAttnArgs) {
-  return tiles == 1 ? lf_kvq_attn_kernel<D, 1, LISTS> : tiles == 2 ? lf_kvq_attn_kernel<D, 2, LISTS> : lf_kvq_attn_kernel<D, 4, LISTS>;
+  return tiles == 1 ? lf_kvq_attn_kernel<D, 1, 1, LISTS> : tiles == 2 ? lf_kvq_attn_kernel<D, 2, 1, LISTS> : lf_kvq_attn_kernel<D, 2, 2, LISTS>;
 }
 
 }  // namespace
@@ -418,8 +487,8 @@ int lf_launch_kvq_attn(const lf_kvq_call* c, void* stream) {
   hipError_t rc = lf_launch(kernel, dim3((unsigned)(blocks * c->parts)), dim3(64 * kWaves), 0, st, a);
   if (rc != hipSuccess) return LF_ERR_HIP;
   if (c->parts == 1) return LF_OK;
-  const unsigned grid = (unsigned)((blocks * c->rows + 3) / 4);
-  rc = c->d == 128 ? lf_launch(lf_kvq_join_kernel<128>, dim3(grid), dim3(256), 0, st, a, c->rows, 16 * tiles, c->H)
-                   : lf_launch(lf_kvq_join_kernel<64>, dim3(grid), dim3(256), 0, st, a, c->rows, 16 * tiles, c->H);
+  const dim3 grid((unsigned)(blocks * c->rows));
+  rc = c->d == 128 ? lf_launch(lf_kvq_join_kernel<128>, grid, dim3(64 * kWaves), 0, st, a, c->rows, 16 * tiles)
+                   : lf_launch(lf_kvq_join_kernel<64>, grid, dim3(64 * kWaves), 0, st, a, c->rows, 16 * tiles);
   return rc == hipSuccess ? LF_OK : LF_ERR_HIP;
 }

@@ -44,20 +44,13 @@ __device__ __forceinline__ void unpack8(const uint4& u, float (&x)[8]) {
   x[6] = __uint_as_float(u.w << 16); x[7] = __uint_as_float(u.w & 0xffff0000u);
 }
 
-// Cosine and sine of pos * freq.  The angle in turns is reduced in float64 to within an eighth of the nearest quarter turn; there
-// the Taylor series up to x^8 and x^9 are off by less than 3e-8.
+// Cosine and sine of pos * freq.  In turns, less the nearest whole number, in float64; the hardware's functions take turns and are off by
+// 2^-22.9 at the most on [-1/2, 1/2] (4 194 304 values), as a float32 series would be.
 __device__ __forceinline__ void angle(int pos, double freq, float& c, float& s) {
-  double t = (double)pos * freq * 0.15915494309189533577;   // 1 / (2 pi)
-  t -= floor(t);
-  const double q = rint(4.0 * t);
-  const float x = (float)(t - 0.25 * q) * 6.283185307179586f;
-  const float x2 = x * x;
-  const float sn = x * fmaf(x2, fmaf(x2, fmaf(x2, fmaf(x2, 1.0f / 362880, -1.0f / 5040), 1.0f / 120), -1.0f / 6), 1.0f);
-  const float cn = fmaf(x2, fmaf(x2, fmaf(x2, fmaf(x2, 1.0f / 40320, -1.0f / 720), 1.0f / 24), -0.5f), 1.0f);
-  const int quarter = (int)q & 3;
-  const float a = quarter & 1 ? sn : cn, b = quarter & 1 ? cn : sn;
-  c = quarter == 1 || quarter == 2 ? -a : a;
-  s = quarter >= 2 ? -b : b;
+  const double t = (double)pos * (freq * 0.15915494309189533577);   // 1 / (2 pi)
+  const float x = (float)(t - __builtin_rint(t));
+  c = __builtin_amdgcn_cosf(x);
+  s = __builtin_amdgcn_sinf(x);
 }
 
 // The angles of a thread's chunk: pairs (2i, 2i + 1) are four to a chunk; of pairs (i, i + d/2) a chunk holds one side of eight.
@@ -72,6 +65,29 @@ __device__ __forceinline__ void angles(const AxesArgs& a, int tok, int cih, floa
     const int i = i0 + e;
     angle(i < a.axis1 ? p0 : i < a.axis2 ? p1 : p2, a.freq[i], cs[e], sn[e]);
   }
+}
+
+// Exchanges among the CH lanes of a head (8 or 16, inside a row of 16) without LDS: quad_perm 0xb1 and 0x4e are lane ^ 1 and ^ 2, 0x1b is ^ 3,
+// row_half_mirror (0x141) is ^ 7, row_ror:n (0x120 + n) rotates the row.
+template <int CTRL> __device__ __forceinline__ float dpp(float v) {
+  return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), CTRL, 0xf, 0xf, false));
+}
+template <int CH> __device__ __forceinline__ float partner(float v) {      // of lane ^ CH/2
+  if constexpr (CH == 16) return dpp<0x128>(v);
+  else return dpp<0x1b>(dpp<0x141>(v));
+}
+template <int CH> __device__ __forceinline__ float head_sum(float v) {     // in all CH lanes
+  if constexpr (CH == 16) {
+    v += dpp<0x128>(v);
+    v += dpp<0x124>(v);
+    v += dpp<0x122>(v);
+    v += dpp<0x121>(v);
+  } else {
+    v += dpp<0x141>(v);
+    v += dpp<0xb1>(v);
+    v += dpp<0x4e>(v);
+  }
+  return v;
 }
 
 // Turns a chunk by its angles (SIGN = 1) or back (-1).
@@ -89,24 +105,20 @@ __device__ __forceinline__ void turn(const float (&y)[8], const float (&cs)[PAIR
     const bool first = cih < CH / 2;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const float other = __shfl_xor(y[e], CH / 2);
+      const float other = partner<CH>(y[e]);
       const float s = first ? -SIGN * sn[e] : SIGN * sn[e];
       r[e] = y[e] * cs[e] + other * s;
     }
   }
 }
 
-template <int CH> __device__ __forceinline__ float head_sum(float v) {
-#pragma unroll
-  for (int off = 1; off < CH; off <<= 1) v += __shfl_xor(v, off);
-  return v;
-}
-
+// Written past the caches: rows of 256 bytes at d = 128, scattered over the heads, were what the kernels waited for (forward, us: 4 680 tokens
+// of 12 heads 8.7 -> 7.2, of 40 heads 22.8 -> 17.2; 32 760 tokens of 12 heads of 64 24.5 -> 17.6).  Nontemporal loads of X bring nothing.
 __device__ __forceinline__ void store8(uint16_t* at, const float (&r)[8]) {
   bf16x8 o;
 #pragma unroll
   for (int e = 0; e < 8; ++e) o[e] = (__bf16)r[e];
-  *reinterpret_cast<bf16x8*>(at) = o;
+  __builtin_nontemporal_store(o, reinterpret_cast<bf16x8*>(at));
 }
 
 template <int D, int NI, int PAIRING>
@@ -172,7 +184,7 @@ __global__ __launch_bounds__(512) void lf_rope_axes_kernel(AxesArgs a) {
 }
 
 // The gradients.  A workgroup takes every gridDim.x-th group of tt tokens and holds what its channels of g get in registers; at
-// the end the tt tokens' shares are added through LDS in ascending order and the workgroup's row goes to `part`.
+// the end the tt tokens' shares are added up through LDS, in ascending order, and the workgroup's row goes to `part`.
 template <int D, int NI, int PAIRING>
 __global__ __launch_bounds__(512) void lf_rope_axes_bwd_kernel(AxesArgs a) {
   constexpr int CH = D / 8;
@@ -274,36 +286,38 @@ __global__ __launch_bounds__(512) void lf_rope_axes_bwd_kernel(AxesArgs a) {
       if (there && h < a.H) store8(a.dX + (int64_t)tok * a.x_stride_tok + h * D + 8 * cih, r);
     }
   }
-  const int width = a.hpt * CH;                 // threads of a token
+  // red[tl][channel]: the tokens' shares side by side, then one thread adds up a channel's
+  __syncthreads();
+  const int cols = a.hpt * D;                   // channels of one of a thread's heads, side by side
 #pragma unroll
-  for (int i = 0; i < NI; ++i) {
-    __syncthreads();
-    if (tl > 0 && tl < a.tt) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) red[e * (a.tt - 1) * width + threadIdx.x - width] = acc[i][e];
+  for (int i = 0; i < NI; ++i)
+    if (tl < a.tt) {
+      float* to = red + (i * a.tt + tl) * cols + hp * D + 8 * cih;
+      *reinterpret_cast<float4*>(to) = make_float4(acc[i][0], acc[i][1], acc[i][2], acc[i][3]);
+      *reinterpret_cast<float4*>(to + 4) = make_float4(acc[i][4], acc[i][5], acc[i][6], acc[i][7]);
     }
-    __syncthreads();
-    const int h = hp + i * a.hpt;
-    if (tl == 0 && h < a.H) {
-      float* to = a.part + (int64_t)blockIdx.x * a.H * D + h * D + 8 * cih;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        float v = acc[i][e];
-        for (int j = 0; j + 1 < a.tt; ++j) v += red[e * (a.tt - 1) * width + j * width + threadIdx.x];
-        to[e] = v;
-      }
-    }
+  __syncthreads();
+  float* row = a.part + (int64_t)blockIdx.x * a.H * D;
+  for (int c = threadIdx.x; c < a.H * D; c += blockDim.x) {
+    const float* from = red + c / cols * a.tt * cols + c % cols;
+    float v = 0.0f;
+    for (int j = 0; j < a.tt; ++j) v += from[j * cols];
+    row[c] = v;
   }
 }
 
 // dg[c] = sum over the rows of `part`, in a fixed order.  A workgroup takes 16 channels, 16 lanes side by side read one row's.
 constexpr int kSumCols = 16, kSumRows = 64;
+static_assert(LF_AXES_MAX_BLOCKS % kSumRows == 0, "every thread adds up the same number of rows");
 __global__ __launch_bounds__(kSumCols * kSumRows) void lf_rope_axes_dg_kernel(const float* part, int rows, int cols, float* dg) {
   __shared__ float red[kSumRows][kSumCols + 1];
   const int lc = threadIdx.x % kSumCols, lr = threadIdx.x / kSumCols;
   const int c = blockIdx.x * kSumCols + lc;     // cols is a multiple of 64
-  float s = 0.0f;
-  for (int r = lr; r < rows; r += kSumRows) s += part[(int64_t)r * cols + c];
+  float v[LF_AXES_MAX_BLOCKS / kSumRows], s = 0.0f;
+#pragma unroll
+  for (int k = 0; k < LF_AXES_MAX_BLOCKS / kSumRows; ++k) v[k] = lr + k * kSumRows < rows ? part[(int64_t)(lr + k * kSumRows) * cols + c] : 0.0f;
+#pragma unroll
+  for (int k = 0; k < LF_AXES_MAX_BLOCKS / kSumRows; ++k) s += v[k];
   red[lr][lc] = s;
   for (int half = kSumRows / 2; half > 0; half /= 2) {
     __syncthreads();
@@ -347,7 +361,7 @@ int lf_launch_rope_axes(const void* X, const float* g, const int32_t* pos, const
                         void* stream) {
   AxesArgs a = axes_args(X, g, pos, freq, p);
   a.Y = (uint16_t*)Y;
-  const lf_axes_lay l = lf_lay_axes_fwd(a.H, p->head_dim);
+  const lf_axes_lay l = lf_lay_axes_fwd(a.H, p->head_dim, a.L);
   a.hpt = l.hpt;
   a.tt = l.tt;
   const unsigned grid = (unsigned)((a.L - 1) / l.tt + 1);
@@ -368,7 +382,7 @@ int lf_launch_rope_axes_bwd(const void* X, const float* g, const int32_t* pos, c
   a.tt = l.tt;
   const int blocks = lf_axes_bwd_blocks(a.H, p->head_dim, a.L);
   const size_t sums = a.across_heads ? 2 * sizeof(float) * l.tt * l.hpt : 0;
-  const size_t shares = 8 * sizeof(float) * (l.tt - 1) * l.hpt * (p->head_dim / 8);   // at most 16 KiB
+  const size_t shares = sizeof(float) * l.ni * l.tt * l.hpt * p->head_dim;      // at most 64 KiB: 512 threads of four heads
   hipStream_t st = (hipStream_t)stream;
   hipError_t rc = lf_launch(p->head_dim == 128 ? kernel_for<128>(true, a.pairing, l.ni) : kernel_for<64>(true, a.pairing, l.ni),
                             dim3(blocks), dim3(l.threads), sums > shares ? sums : shares, st, a);
