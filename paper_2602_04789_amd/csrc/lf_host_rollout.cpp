@@ -82,7 +82,7 @@ int check_token(const lf_token_shape* s) {
 }
 
 int token_parts(const lf_token_shape* s) {
-  return lf_kvq_parts_of(s->heads, ((int64_t)s->cached_len + 63) / 64 + ((int64_t)s->extra_len + 63) / 64);
+  return lf_kvq_parts_of(s->heads, ((int64_t)s->cached_len + 63) / 64 + ((int64_t)s->extra_len + 63) / 64, s->q_len);
 }
 
 // The call's sizes, its strides apart: those of K and V are asked for only where there are K and V.
@@ -162,8 +162,8 @@ extern "C" size_t lf_sparse_attn_kvq_workspace_bytes(const lf_shape* s, int32_t 
   lf_dims dm;
   if (check_lists(s, list_len, &dm) != LF_OK) return 0;
   const int64_t blocks = (int64_t)dm.H * dm.n_q;
-  if (lf_kvq_expands(dm.d, blocks, list_len, dm.H, s->kv_len)) return 2 * expanded_bytes(dm);
-  return (size_t)lf_kvq_state_bytes(blocks, lf_kvq_parts_of(blocks, list_len), list_rows(dm), dm.d);
+  if (lf_kvq_expands(dm.d, blocks, list_len, list_rows(dm), dm.H, s->kv_len)) return 2 * expanded_bytes(dm);
+  return (size_t)lf_kvq_state_bytes(blocks, lf_kvq_parts_of(blocks, list_len, list_rows(dm)), list_rows(dm), dm.d);
 }
 
 extern "C" int lf_sparse_attn_kvq(const void* Q, const void* cache, size_t cache_bytes, const lf_kvq_shape* cs, const void* K,
@@ -202,7 +202,7 @@ extern "C" int lf_sparse_attn_kvq(const void* Q, const void* cache, size_t cache
   c.extra = s->kv_len - cached;
   c.rows = list_rows(dm);
   const int64_t blocks = (int64_t)dm.H * dm.n_q;
-  if (lf_kvq_expands(dm.d, blocks, list_len, dm.H, s->kv_len)) {
+  if (lf_kvq_expands(dm.d, blocks, list_len, list_rows(dm), dm.H, s->kv_len)) {
     uint16_t *Kw = (uint16_t*)workspace, *Vw = (uint16_t*)((char*)workspace + expanded_bytes(dm));
     if ((rc = lf_launch_kvq_expand(&c, Kw, Vw, stream)) != LF_OK) return rc;
     lf_shape t = *s;
@@ -210,7 +210,7 @@ extern "C" int lf_sparse_attn_kvq(const void* Q, const void* cache, size_t cache
     t.k_stride_head = t.v_stride_head = (int64_t)s->kv_len * dm.d;
     return lf_launch_attn(Q, Kw, Vw, &t, &dm, indices, list_len, list_len, c.scale, O, nullptr, nullptr, nullptr, stream);
   }
-  c.parts = lf_kvq_parts_of(blocks, list_len);
+  c.parts = lf_kvq_parts_of(blocks, list_len, c.rows);
   c.workspace = workspace;
   return lf_launch_kvq_attn(&c, stream);
 }

@@ -13,9 +13,9 @@
 // so P stays in its registers; V goes through LDS as bfloat16 rows and comes back by the transposing read.  The bytes of
 // the next tile are requested as soon as those of the present one are converted.
 //
-// Softmax is float32 in the exp2 domain, P = exp2(s c - m), against a reference m per row that moves only when a P passes 2^8: without
-// that no lane asks another and no maximum of scores is taken.  P is rounded to bfloat16 for the product (as the output is); the row's sum
-// is the product of the same P with ones, in float32.
+// Softmax is float32 in the exp2 domain, P = exp2(s c - m), against a reference m per row that moves only when a tile's sum of P is large:
+// without that no lane asks another and no maximum of scores is taken.  P is rounded to bfloat16 for the product (as the output is); the
+// row's sum is the product of the same P with ones, in float32.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -47,7 +47,7 @@ struct KvqAttnArgs {
 };
 
 constexpr int kWaves = 4;
-constexpr float kMostP = 256.0f;    // a larger P moves the reference
+constexpr float kMostSum = 16384.0f;  // a larger sum of a tile's P moves the reference: P is 2^8 on the mean then, far from overflow
 
 #define LDS_PTR(T, p) ((__attribute__((address_space(3))) T*)(p))
 
@@ -141,11 +141,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void lf_kvq_attn_kernel(KvqAttnArgs
   // The bytes of a tile: a lane's D/4 channels of four tokens of K, and its groups of V, half a tile at a time.
   uint32_t kw[4][CW], ksc[4], vw[2][VI][4], vsc[2][VI];
   auto load_k = [&](const Tile& t) __attribute__((always_inline)) {
-    if (t.cnt == 0) return;
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
       const int row = t.tok + min(16 * s + col, t.cnt - 1);
-      const uint8_t* p = kc + (uint32_t)row * (D / 2) + (D / 8) * kg;
+      const uint8_t* p = kc + (uint32_t)(row * (D / 2) + (D / 8) * kg);
       if constexpr (CW == 4) {
         const uint4 x = *reinterpret_cast<const uint4*>(p);
         kw[s][0] = x.x; kw[s][1] = x.y; kw[s][2] = x.z; kw[s][3] = x.w;
@@ -153,41 +152,39 @@ __global__ __launch_bounds__(64 * kWaves, 2) void lf_kvq_attn_kernel(KvqAttnArgs
         const uint2 x = *reinterpret_cast<const uint2*>(p);
         kw[s][0] = x.x; kw[s][1] = x.y;
       }
-      ksc[s] = ks[(uint32_t)row * (D / 32) + (D == 128 ? kg : kg >> 1)];
+      ksc[s] = ks[(uint32_t)(row * (D / 32) + (D == 128 ? kg : kg >> 1))];
     }
   };
   auto load_v = [&](const Tile& t, int half) __attribute__((always_inline)) {
-    if (t.cnt == 0) return;
 #pragma unroll
     for (int i = 0; i < VI; ++i) {
       const int item = 64 * i + lane, row = t.tok + min(32 * half + item / (D / 32), t.cnt - 1), grp = item % (D / 32);
-      const uint4 x = *reinterpret_cast<const uint4*>(vc + (uint32_t)row * (D / 2) + 16 * grp);
+      const uint4 x = *reinterpret_cast<const uint4*>(vc + (uint32_t)(row * (D / 2) + 16 * grp));
       vw[half][i][0] = x.x; vw[half][i][1] = x.y; vw[half][i][2] = x.z; vw[half][i][3] = x.w;
-      vsc[half][i] = vs[(uint32_t)row * (D / 32) + grp];
+      vsc[half][i] = vs[(uint32_t)(row * (D / 32) + grp)];
     }
   };
 
   f32x4 oacc[NQ][MB];
-  f32x4 lacc[NQ];               // row sums: the product of P with ones, the same in every row of the result
-  float m_run[NQ];
+  float m_run[NQ], l_run[NQ];
   bool first = true;
 #pragma unroll
   for (int q = 0; q < NQ; ++q) {
     m_run[q] = -INFINITY;
-    lacc[q] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    l_run[q] = 0.0f;
 #pragma unroll
     for (int mb = 0; mb < MB; ++mb) oacc[q][mb] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   }
   bf16x8 ones;
 #pragma unroll
   for (int i = 0; i < 8; ++i) ones[i] = (__bf16)1.0f;
-  // Rows of V in LDS: the transposing read takes 32 bytes of four rows at a time, which land in different banks when the row's two low bits
-  // go to the chunk's high bits (d = 128) or its second bit does (d = 64).
-  auto swz = [](int row, int ch) __attribute__((always_inline)) { return CH == 16 ? ch ^ ((row & 3) << 2) : ch ^ (((row >> 1) & 1) << 2); };
+  // Rows of V in LDS, 16-byte chunks swizzled so that neither side meets a bank twice: 16 lanes write one chunk (u) of every group of four rows
+  // (d = 64: eight), 32 lanes of the transposing read take 32 bytes (two chunks) of each of eight rows.  Pairs of chunks go by the row, the place
+  // in a pair by the group; 16 rows on it is the same.
+  auto swz = [](int row, int ch) __attribute__((always_inline)) {
+    return ch ^ (CH == 16 ? (row & 7) << 1 : (row >> 1 & 3) << 1) ^ (ch >> 2 & 1);
+  };
   u32x4* vt = stage[wave];
-  // A lane writes the four chunks of its group in an order of its own: in one order all lanes would write the same quarter of the banks at a time.
-  const int rot = lane >> 2 & 3;
-  const bool rot1 = lane & 4, rot2 = lane & 8;
   auto own_lds = []() __attribute__((always_inline)) {    // this wavefront's own rows: LDS keeps its order, and the compiler its own
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
     __builtin_amdgcn_wave_barrier();
@@ -203,21 +200,16 @@ __global__ __launch_bounds__(64 * kWaves, 2) void lf_kvq_attn_kernel(KvqAttnArgs
         const int item = 64 * i + lane, row = item / (D / 32), grp = item % (D / 32);
         u32x4 y[4];
         if constexpr (!EXT) {
-          uint32_t x[4], z[4];
 #pragma unroll
-          for (int u = 0; u < 4; ++u) x[u] = rot1 ? vw[half][i][(u + 1) & 3] : vw[half][i][u];
-#pragma unroll
-          for (int u = 0; u < 4; ++u) z[u] = rot2 ? x[(u + 2) & 3] : x[u];
-#pragma unroll
-          for (int u = 0; u < 4; ++u) y[u] = decode(z[u], scale_of(vsc[half][i])).x;
+          for (int u = 0; u < 4; ++u) y[u] = decode(vw[half][i][u], scale_of(vsc[half][i])).x;
         } else {
           const int tok = cur.tok + min(32 * half + row, cur.cnt - 1);
           const uint16_t* p = a.Vx + (int64_t)h * a.v_stride_head + (int64_t)tok * a.v_stride_tok + 32 * grp;
 #pragma unroll
-          for (int u = 0; u < 4; ++u) y[u] = *reinterpret_cast<const u32x4*>(p + 8 * ((u + rot) & 3));
+          for (int u = 0; u < 4; ++u) y[u] = *reinterpret_cast<const u32x4*>(p + 8 * u);
         }
 #pragma unroll
-        for (int u = 0; u < 4; ++u) vt[row * CH + swz(row, 4 * grp + ((u + rot) & 3))] = y[u];
+        for (int u = 0; u < 4; ++u) vt[row * CH + swz(row, 4 * grp + u)] = y[u];
       }
       own_lds();
       if constexpr (!EXT) load_v(then, half);
@@ -254,7 +246,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void lf_kvq_attn_kernel(KvqAttnArgs
             if (16 * s + 4 * kg + i >= cur.cnt) sacc[q][s][i] = -INFINITY;
     }
     // P against the reference as it stands; where that is too low (or not set yet: the wavefront's first tile) it moves up to the maxima and P
-    // is made again.
+    // is made again, before it has gone into any sum.
     float p[NQ][16];
     auto weights = [&]() __attribute__((always_inline)) {
 #pragma unroll
@@ -262,15 +254,26 @@ __global__ __launch_bounds__(64 * kWaves, 2) void lf_kvq_attn_kernel(KvqAttnArgs
 #pragma unroll
         for (int i = 0; i < 16; ++i) p[q][i] = __builtin_amdgcn_exp2f(fmaf(sacc[q][i >> 2][i & 3], a.c, -m_run[q]));
     };
+    bf16x8 pf[NQ][2];
+    f32x4 sum[NQ];
+    auto sums = [&]() __attribute__((always_inline)) {
+#pragma unroll
+      for (int q = 0; q < NQ; ++q) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) pf[q][i >> 3][i & 7] = (__bf16)p[q][i];
+        sum[q] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int half = 0; half < 2; ++half) sum[q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pf[q][half], sum[q], 0, 0, 0);
+      }
+    };
     bool move = first;
     if (!first) {
       weights();
-      float most = 0.0f;
+      sums();
+      bool past = false;
 #pragma unroll
-      for (int q = 0; q < NQ; ++q)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) most = fmaxf(most, p[q][i]);
-      move = __ballot(most > kMostP) != 0ull;
+      for (int q = 0; q < NQ; ++q) past = past || sum[q][0] > kMostSum;
+      move = __ballot(past) != 0ull;
     }
     if (move) {
 #pragma unroll
@@ -283,25 +286,18 @@ __global__ __launch_bounds__(64 * kWaves, 2) void lf_kvq_attn_kernel(KvqAttnArgs
         const float m_new = first ? top : fmaxf(m_run[q], top);
         const float alpha = first ? 0.0f : __builtin_amdgcn_exp2f(m_run[q] - m_new);
         m_run[q] = m_new;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) lacc[q][i] *= alpha;
+        l_run[q] *= alpha;
 #pragma unroll
         for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
           for (int i = 0; i < 4; ++i) oacc[q][mb][i] *= alpha;
       }
       weights();
+      sums();
       first = false;
     }
-    bf16x8 pf[NQ][2];
 #pragma unroll
-    for (int q = 0; q < NQ; ++q)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) pf[q][i >> 3][i & 7] = (__bf16)p[q][i];
-#pragma unroll
-    for (int q = 0; q < NQ; ++q)
-#pragma unroll
-      for (int half = 0; half < 2; ++half) lacc[q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pf[q][half], lacc[q], 0, 0, 0);
+    for (int q = 0; q < NQ; ++q) l_run[q] += sum[q][0];
     auto product = [&](int half) __attribute__((always_inline)) {
       const uint16_t* v16 = reinterpret_cast<const uint16_t*>(vt);
 #pragma unroll
@@ -321,12 +317,15 @@ __global__ __launch_bounds__(64 * kWaves, 2) void lf_kvq_attn_kernel(KvqAttnArgs
   };
   begin();
   Tile cur = next(false);
-  load_k(cur);
-  load_v(cur, 0);
-  load_v(cur, 1);
+  if (cur.cnt > 0) {
+    load_k(cur);
+    load_v(cur, 0);
+    load_v(cur, 1);
+  }
   while (cur.cnt > 0) {
     const Tile then = next(false);
-    tile(std::false_type{}, cur, then);
+    // behind the last tile it is requested once more: loads that depend on a branch would make the waits of every tile wait for all of them
+    tile(std::false_type{}, cur, then.cnt > 0 ? then : cur);
     cur = then;
   }
   if (a.extra > 0) {
@@ -337,7 +336,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void lf_kvq_attn_kernel(KvqAttnArgs
   // The states of the SL wavefronts that have the same rows become one.
 #pragma unroll
   for (int q = 0; q < NQ; ++q) {
-    if (kg == 0) ml[wave][16 * q + col] = make_float2(m_run[q], lacc[q][0]);
+    if (kg == 0) ml[wave][16 * q + col] = make_float2(m_run[q], l_run[q]);
   }
   __syncthreads();
   f32x4* buf = reinterpret_cast<f32x4*>(&stage[0][0]);        // MB tiles of four wavefronts, 64 lanes each: the whole stage

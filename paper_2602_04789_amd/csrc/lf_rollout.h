@@ -77,17 +77,31 @@ struct lf_kvq_call {
 inline int lf_kvq_tiles(int rows) { return rows <= 16 ? 1 : rows <= 32 ? 2 : 4; }
 #define LF_KVQ_MAX_PARTS 64     // a lane of the joining wavefront each
 // Into how many workgroups of four wavefronts the list of a query block is divided: until every compute unit has two, as long as each
-// wavefront has a KV block.
-inline int lf_kvq_parts_of(int64_t blocks, int64_t entries) {
-  int64_t p = blocks > 0 ? 512 / blocks : 1;
+// wavefront has a KV block.  Lists that give the wavefronts of one workgroup (with more than 32 rows two share a block) four blocks at the
+// most stay whole: joining the parts costs more than it brings.  us, divided / whole: 12 heads of 128, one row, 501 tokens 8.9 / 7.2, 701 7.6 / 7.3,
+// 1 001 (17 blocks) 8.9 / 9.7, 1 401 9.0 / 11.1; 40 heads of 64, 701 6.5 / 5.8; 8 query blocks of 64 rows, lists of 12 9.2 / 10.4.
+inline int lf_kvq_parts_of(int64_t blocks, int64_t entries, int rows) {
+  if (entries <= (rows > 32 ? 8 : 16)) return 1;
+  int64_t p = 512 / blocks;
   if (p > entries / 4) p = entries / 4;
   return (int)(p < 1 ? 1 : p > LF_KVQ_MAX_PARTS ? LF_KVQ_MAX_PARTS : p);
 }
-// Whether a call with lists first writes the cache's rows in bfloat16 and runs the bfloat16 kernels on them.  That costs its time for every
-// token of the cache (1.4 us a million values), the kernel that converts what it reads pays for every tile of 64 x 64 (2.0 ns more at d = 128, 1.2 at
-// d = 64).
-inline bool lf_kvq_expands(int d, int64_t blocks, int64_t entries, int64_t H, int64_t kv_len) {
-  return blocks * entries * (d == 128 ? 1470 : 860) > H * kv_len * d + 700000;
+// Whether a call with lists first writes the cache's rows in bfloat16 and runs the bfloat16 kernels on them.  That costs time for every value
+// of the cache, whatever the lists keep, and these kernels do not divide a list among workgroups; the kernel that converts what it reads pays for that at
+// every tile, once for every query block.  Up to 256 query blocks both sides' times (us) are put together from what they are made of,
+// beyond, tiles are weighed against values.  8 340 random calls (1 to 40 heads, frames of 8 to 1 600 tokens, lists of 1 to 3 000 blocks), both ways each:
+// this choice costs 0.9 % on the mean over the faster one (0.6 at the worst call), the bfloat16 kernels always 33 % (6.1), the converting one always 12 % (1.7).
+inline bool lf_kvq_expands(int d, int64_t blocks, int64_t entries, int rows, int64_t H, int64_t kv_len) {
+  const int64_t values = H * kv_len * d;
+  const bool wide = d == 128;
+  if (blocks > 256) return blocks * entries * (wide ? 1400 : 750) > values;
+  const int parts = lf_kvq_parts_of(blocks, entries, rows), at_once = parts * (rows > 32 ? 2 : 4);
+  const double tiles = (double)((entries + at_once - 1) / at_once);
+  double convert = (wide ? 4.7 : 4.2) + tiles * (blocks * parts <= 256 ? (wide ? 1.8 : 1.2) : (wide ? 2.8 : 1.8));
+  if (parts > 1) convert += (wide ? 3.9 : 3.2) + blocks * rows * (wide ? 0.0024 : 0.0014);
+  const double expand = (wide ? 9.1 : 8.7) + values * 1.35e-6 +
+                        entries * (blocks <= 128 ? (wide ? 0.267 : 0.146) : (wide ? 0.505 : 0.334));
+  return expand < convert;
 }
 // Float32 state of the parts: O [H n_q][parts][16 tiles][d], then (reference, sum) [H n_q][parts][16 tiles][2].
 inline int64_t lf_kvq_state_bytes(int64_t blocks, int parts, int rows, int d) {
