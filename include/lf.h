@@ -400,8 +400,8 @@ int lf_qk_norm_rope(const void* X, const float* g, const float* cos_table, const
  *   dg       device, float32 [H*d], written.
  *   workspace  device scratch of >= lf_qk_norm_rope_axes_bwd_workspace_bytes(), 256-byte aligned.
  *   X, Y, dY, dX, g 16-byte aligned, freq 8, pos and dg 4; strides multiples of 8.  Y must not overlap X.
- * Errors: LF_ERR_NULL, LF_ERR_SHAPE (as lf_qk_norm_rope; H*d above 16 384; pairs negative or not adding up to d/2),
- *   LF_ERR_ALIGN, LF_ERR_WORKSPACE, LF_ERR_HIP.
+ * Errors: LF_ERR_NULL, LF_ERR_SHAPE (as lf_qk_norm_rope; H*d above 16 384; pairs negative or not adding up to d/2; more
+ *   than 2^32 threads' worth of tokens, some 10^11 values), LF_ERR_ALIGN, LF_ERR_WORKSPACE, LF_ERR_HIP.
  */
 typedef struct {
   int32_t heads;        /* H */

@@ -95,7 +95,8 @@ def build(verbose: bool = False, extra_device_flags=()) -> str:
     return LIB
 
 
-def build_sanitized_host(out_dir: str = OBJ) -> str:
+def build_sanitized_host(out_dir: str = OBJ, sources=("lf_host.cpp",), driver: str = "host_sanitize_driver.cpp",
+                         name: str = "lf_host_sanitized") -> str:
     """Host side of the C ABI alone (lf_host.cpp: validation, budgets, sizes) compiled for the CPU
     with AddressSanitizer and UndefinedBehaviorSanitizer, linked with the test driver that stands
     in for the kernel launchers.  Returns the executable's path; no GPU code is involved."""
@@ -103,11 +104,11 @@ def build_sanitized_host(out_dir: str = OBJ) -> str:
     if not gxx:
         raise RuntimeError("g++ not found")
     os.makedirs(out_dir, exist_ok=True)
-    exe = os.path.join(out_dir, "lf_host_sanitized")
+    exe = os.path.join(out_dir, name)
     _run([gxx, "-std=c++17", "-O1", "-g", "-fsanitize=address,undefined", "-fno-sanitize-recover=all",
           "-fno-omit-frame-pointer", "-ffp-contract=off", "-Wall", "-I", os.path.join(ROOT, "include"),
-          "-I", CSRC, os.path.join(CSRC, "lf_host.cpp"),
-          os.path.join(ROOT, "tests", "host_sanitize_driver.cpp"), "-o", exe])
+          "-I", CSRC] + [os.path.join(CSRC, src) for src in sources] +
+         [os.path.join(ROOT, "tests", driver), "-o", exe])
     return exe
 
 

@@ -454,4 +454,4 @@ extern "C" const char* lf_strerror(int status) {
   }
 }
 
-extern "C" int lf_version(void) { return 200; }
+extern "C" int lf_version(void) { return 300; }

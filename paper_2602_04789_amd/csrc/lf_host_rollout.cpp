@@ -37,7 +37,8 @@ int check_axes(const lf_axes_shape* p) {
   if (!(p->eps >= 0.0f) || isinf(p->eps)) return LF_ERR_SHAPE;
   if (p->x_stride_tok < (int64_t)p->heads * p->head_dim || p->y_stride_tok < p->head_dim || p->y_stride_head < 0) return LF_ERR_SHAPE;
   if (p->x_stride_tok % 8 || p->y_stride_tok % 8 || p->y_stride_head % 8) return LF_ERR_ALIGN;
-  return LF_OK;
+  const lf_axes_lay l = lf_lay_axes_fwd(p->heads, p->head_dim, p->tokens);       // a grid has less than 2^32 threads
+  return ((int64_t)(p->tokens - 1) / l.tt + 1) * l.threads < (int64_t)1 << 32 ? LF_OK : LF_ERR_SHAPE;
 }
 
 bool axes_misaligned(const void* X, const float* g, const int32_t* pos, const double* freq) {

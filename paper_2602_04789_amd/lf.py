@@ -590,12 +590,13 @@ def _axes_shape(X, g, pos, freq, pairs, heads, rows, eps, across_heads, pairing)
     if freq.dtype is not torch.float64 or not freq.is_contiguous():
         raise ValueError("freq must be contiguous float64 [d / 2]")
     (yheads, tokens, d), yt, yh = rows
+    heads = int(heads)
     xs, xsh = X.stride(), X.shape
     if len(xs) != 2 or xs[1] != 1 or xsh[0] != tokens or yheads != heads:
         raise ValueError("X must be [L, >= H * d] with contiguous channels, Y and dY [H, L, d]")
     if xsh[1] < heads * d or g.numel() != heads * d or pos.shape != (tokens, 3) or freq.numel() != d // 2 or len(pairs) != 3:
         raise ValueError("shapes of X, g, pos, freq or pairs do not fit")
-    return lf_axes_shape(heads, d, tokens, 1 if across_heads else 0, pairing, tuple(pairs), eps, 0,
+    return lf_axes_shape(heads, d, tokens, 1 if across_heads else 0, int(pairing), (int(pairs[0]), int(pairs[1]), int(pairs[2])), float(eps), 0,
                          xs[0] if tokens != 1 else heads * d, yt, yh)
 
 
@@ -615,8 +616,8 @@ def lf_qk_norm_rope_axes(X, g, pos, freq, pairs, heads: int, Y, eps: float = 1e-
 
 
 def lf_qk_norm_rope_axes_bwd_workspace_bytes(heads: int, head_dim: int, tokens: int) -> int:
-    p = lf_axes_shape(heads, head_dim, tokens, 0, 0, (C.c_int32 * 3)(head_dim // 2, 0, 0), 0.0, 0, heads * head_dim, head_dim,
-                      tokens * head_dim)
+    H, d, L = int(heads), int(head_dim), int(tokens)
+    p = lf_axes_shape(H, d, L, 0, 0, (d // 2, 0, 0), 0.0, 0, H * d, d, L * d)
     return int(load().lf_qk_norm_rope_axes_bwd_workspace_bytes(C.byref(p)))
 
 
@@ -632,8 +633,10 @@ def lf_qk_norm_rope_axes_bwd(X, g, pos, freq, pairs, heads: int, dY, eps: float 
     if grads is None:
         tokens, row = p.tokens, X.stride(0)
         dg = _new(g.shape, torch.float32, X, stream)
-        dX = _new(X.shape, torch.bfloat16, X, stream) if tokens == 1 or row == X.shape[1] else \
-            _new(tokens * row, torch.bfloat16, X, stream).as_strided(X.shape, X.stride())
+        if tokens == 1 or row == X.shape[1]:
+            dX = _new(X.shape, torch.bfloat16, X, stream)
+        else:
+            dX = _new(tokens * row, torch.bfloat16, X, stream).as_strided(X.shape, X.stride())
     else:
         dX, dg = grads
         if dX.dtype is not torch.bfloat16 or dX.shape != X.shape or dX.stride(1) != 1 or (dX.shape[0] != 1 and dX.stride(0) != X.stride(0)):
@@ -652,7 +655,7 @@ def lf_qk_norm_rope_axes_bwd(X, g, pos, freq, pairs, heads: int, dY, eps: float 
 
 def lf_kvq_bytes(heads: int, head_dim: int, capacity: int) -> int:
     """Bytes of a 4-bit cache for `capacity` tokens (0 on bad input)."""
-    return int(load().lf_kvq_bytes(C.byref(lf_kvq_shape(heads, head_dim, capacity, 0))))
+    return int(load().lf_kvq_bytes(C.byref(lf_kvq_shape(int(heads), int(head_dim), int(capacity), 0))))
 
 
 def lf_kvq_append(K, V, cache, capacity: int, first: int, stream=None):
@@ -664,8 +667,8 @@ def lf_kvq_append(K, V, cache, capacity: int, first: int, stream=None):
         raise ValueError("K and V must have one shape")
     at, st = _here(stream)
     _one_device(at, (K, V, cache))
-    rc = (_lib or load()).lf_kvq_append(K.data_ptr(), V.data_ptr(), C.byref(lf_kvq_shape(sh[0], sh[2], capacity)),
-                                        C.byref(lf_kvq_rows(first, sh[1], kt, kh, vt, vh)), cache.data_ptr(), cache.numel(), st)
+    rc = (_lib or load()).lf_kvq_append(K.data_ptr(), V.data_ptr(), C.byref(lf_kvq_shape(sh[0], sh[2], int(capacity))),
+                                        C.byref(lf_kvq_rows(int(first), sh[1], kt, kh, vt, vh)), cache.data_ptr(), cache.numel(), st)
     if rc != LF_OK:
         raise LfError(rc, "lf_kvq_append")
     return cache
@@ -675,7 +678,7 @@ def lf_kvq_read(cache, heads: int, head_dim: int, capacity: int, first: int, tok
     """The values that tokens [first, first + tokens) of the 4-bit cache stand for: (K, V), bfloat16 [H, tokens, d]."""
     torch = _torch or _get_torch()
     _check_buffer(cache, "cache")
-    shape = (heads, tokens, head_dim)
+    shape = heads, tokens, d = int(heads), int(tokens), int(head_dim)
     if K is None:
         K = _new(shape, torch.bfloat16, cache, stream)
     if V is None:
@@ -685,8 +688,8 @@ def lf_kvq_read(cache, heads: int, head_dim: int, capacity: int, first: int, tok
         raise ValueError("K and V must be [H, tokens, d]")
     at, st = _here(stream)
     _one_device(at, (cache, K, V))
-    rc = (_lib or load()).lf_kvq_read(cache.data_ptr(), cache.numel(), C.byref(lf_kvq_shape(heads, head_dim, capacity)),
-                                      C.byref(lf_kvq_rows(first, tokens, kt, kh, vt, vh)), K.data_ptr(), V.data_ptr(), st)
+    rc = (_lib or load()).lf_kvq_read(cache.data_ptr(), cache.numel(), C.byref(lf_kvq_shape(heads, d, int(capacity))),
+                                      C.byref(lf_kvq_rows(int(first), tokens, kt, kh, vt, vh)), K.data_ptr(), V.data_ptr(), st)
     if rc != LF_OK:
         raise LfError(rc, "lf_kvq_read")
     return K, V
@@ -695,8 +698,8 @@ def lf_kvq_read(cache, heads: int, head_dim: int, capacity: int, first: int, tok
 def lf_sparse_attn_kvq_workspace_bytes(heads: int, head_dim: int, frame_len: int, block: int, q_len: int, kv_len: int,
                                        list_len: int) -> int:
     d = int(head_dim)
-    sh = lf_shape(heads, d, frame_len, block, q_len, kv_len, LF_BF16, 0, d, 0, d, 0, d, 0, d, 0)
-    return int(load().lf_sparse_attn_kvq_workspace_bytes(C.byref(sh), list_len))
+    sh = lf_shape(int(heads), d, int(frame_len), int(block), int(q_len), int(kv_len), LF_BF16, 0, d, 0, d, 0, d, 0, d, 0)
+    return int(load().lf_sparse_attn_kvq_workspace_bytes(C.byref(sh), int(list_len)))
 
 
 def lf_sparse_attn_kvq(Q, cache, capacity: int, kv_len: int, indices, frame_len: int, block: int, K=None, V=None,
@@ -723,13 +726,13 @@ def lf_sparse_attn_kvq(Q, cache, capacity: int, kv_len: int, indices, frame_len:
         raise ValueError("K and V go together")
     else:
         _one_device(at, (Q, cache, indices, O))
-    sh = lf_shape(heads, d, frame_len, block, q_len, kv_len, LF_BF16, 0, qt, qh, kt, kh, vt, vh, ot, oh)
-    _check_lists(indices, sh, frame_len)
+    sh = lf_shape(heads, d, int(frame_len), int(block), q_len, int(kv_len), LF_BF16, 0, qt, qh, kt, kh, vt, vh, ot, oh)
+    _check_lists(indices, sh, sh.frame_len)
     length = indices.shape[2]
     lib = _lib or load()
     ws = _workspace(workspace, lambda: lib.lf_sparse_attn_kvq_workspace_bytes(C.byref(sh), length), Q, stream, at)
-    rc = lib.lf_sparse_attn_kvq(Q.data_ptr(), cache.data_ptr(), cache.numel(), C.byref(lf_kvq_shape(heads, d, capacity)),
-                                k_ptr, v_ptr, C.byref(sh), indices.data_ptr(), length, softmax_scale, O.data_ptr(), *_bytes_of(ws), st)
+    rc = lib.lf_sparse_attn_kvq(Q.data_ptr(), cache.data_ptr(), cache.numel(), C.byref(lf_kvq_shape(heads, d, int(capacity))),
+                                k_ptr, v_ptr, C.byref(sh), indices.data_ptr(), length, float(softmax_scale), O.data_ptr(), *_bytes_of(ws), st)
     if rc != LF_OK:
         raise LfError(rc, "lf_sparse_attn_kvq")
     return O
@@ -737,7 +740,7 @@ def lf_sparse_attn_kvq(Q, cache, capacity: int, kv_len: int, indices, frame_len:
 
 def lf_token_attn_kvq_workspace_bytes(heads: int, head_dim: int, q_len: int, cached_len: int, extra_len: int) -> int:
     d = int(head_dim)
-    sh = lf_token_shape(heads, d, q_len, cached_len, extra_len, 0, d, 0, d, 0, d, 0, d, 0)
+    sh = lf_token_shape(int(heads), d, int(q_len), int(cached_len), int(extra_len), 0, d, 0, d, 0, d, 0, d, 0)
     return int(load().lf_token_attn_kvq_workspace_bytes(C.byref(sh)))
 
 
@@ -766,11 +769,11 @@ def lf_token_attn_kvq(Q, cache, capacity: int, cached_len: int, K=None, V=None, 
         raise ValueError("K and V go together")
     else:
         _one_device(at, (Q, cache, O))
-    sh = lf_token_shape(heads, d, q_len, cached_len, extra, 0, qt, qh, kt, kh, vt, vh, ot, oh)
+    sh = lf_token_shape(heads, d, q_len, int(cached_len), extra, 0, qt, qh, kt, kh, vt, vh, ot, oh)
     lib = _lib or load()
     ws = _workspace(workspace, lambda: lib.lf_token_attn_kvq_workspace_bytes(C.byref(sh)), Q, stream, at)
-    rc = lib.lf_token_attn_kvq(Q.data_ptr(), cache.data_ptr(), cache.numel(), C.byref(lf_kvq_shape(heads, d, capacity)),
-                               k_ptr, v_ptr, C.byref(sh), softmax_scale, O.data_ptr(), *_bytes_of(ws), st)
+    rc = lib.lf_token_attn_kvq(Q.data_ptr(), cache.data_ptr(), cache.numel(), C.byref(lf_kvq_shape(heads, d, int(capacity))),
+                               k_ptr, v_ptr, C.byref(sh), float(softmax_scale), O.data_ptr(), *_bytes_of(ws), st)
     if rc != LF_OK:
         raise LfError(rc, "lf_token_attn_kvq")
     return O

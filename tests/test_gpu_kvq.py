@@ -336,3 +336,40 @@ def test_binding_refuses(gpu):
                  lambda: lf.lf_sparse_attn_kvq(Q, cache, T, 3 * 64, idx, 64, 64), lambda: lf.lf_kvq_read(cache, H, d, T, 127, 2)):
         with pytest.raises(lf.LfError):
             call()
+
+
+@pytest.mark.parametrize("H,n,f,F,length", [(2, 70, 1, 8, 6), (40, 70, 2, 6, 12)])
+def test_what_no_list_keeps_may_be_anything(gpu, H, n, f, F, length):
+    """NaN and infinities in the cache right behind the tokens of listed blocks, and in the blocks that no list holds, in both ways."""
+    torch, lf = gpu
+    d, nb, kv, q = 64, 2, F * n, f * n
+    K, V = _rand(torch, 1, H, kv, d), _rand(torch, 2, H, kv, d)
+    Q = _rand(torch, 3, H, q, d)
+    keep = torch.tensor([c for c in range(F * nb) if c % 3 != 1])          # 0, 2, 3, 5, ...: whole blocks and short ones
+    for c in range(F * nb):
+        if c % 3 == 1:
+            t = torch.from_numpy(R.block_tokens([c], n, nb, F * nb))
+            K[:, t, 5], V[:, t, 7] = float("nan"), float("inf")
+    dev, host = _cache(gpu, H, kv, d, K, V)
+    g = torch.Generator().manual_seed(4)
+    idx = torch.stack([keep[torch.randperm(len(keep), generator=g)[:length]] for _ in range(H * f * nb)]).to(torch.int32).view(H, f * nb, -1)
+    O = _np(lf.lf_sparse_attn_kvq(Q.cuda(), dev, kv, kv, idx.cuda(), n, 64))
+    rk, rv = R.cache_read(host, H, kv, d, 0, kv)
+    for h in range(H):
+        for r in range(f * nb):
+            rows, t = R.block_tokens([r], n, nb, f * nb), R.block_tokens(idx[h, r].tolist(), n, nb, F * nb)
+            _check(O[h, rows], _np(Q[h])[rows], rk[h, t], rv[h, t], d ** -0.5)
+
+
+def test_a_value_that_is_not_finite_stays_in_its_heads_rows(gpu):
+    """One NaN among the keys or the values: all rows of that head (its channels, for a value's) are NaN, other heads are as they were."""
+    torch, lf = gpu
+    H, d, T = 3, 128, 300
+    K, V, Q = _rand(torch, 1, H, T, d), _rand(torch, 2, H, T, d), _rand(torch, 3, H, 4, d).cuda()
+    dev, _ = _cache(gpu, H, T, d, K, V)
+    want = lf.lf_token_attn_kvq(Q, dev, T, T).clone()
+    K[1, 170, 3], V[2, 11, 40] = float("inf"), float("nan")
+    dev, _ = _cache(gpu, H, T, d, K, V)
+    got = lf.lf_token_attn_kvq(Q, dev, T, T)
+    assert torch.equal(got[0], want[0]) and torch.isnan(got[1]).all() and torch.isnan(got[2, :, 32:64]).all()
+    assert torch.equal(got[2, :, :32], want[2, :, :32]) and torch.equal(got[2, :, 64:], want[2, :, 64:])

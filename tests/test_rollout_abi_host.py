@@ -191,3 +191,15 @@ def test_binding_refuses_wrong_tensors():
                  lambda: lf.lf_sparse_attn_kvq(Y, cache, 8, 8, pos, 4, 64)):
         with pytest.raises(ValueError):
             call()
+
+
+def test_host_side_under_address_and_undefined_behaviour_sanitizers(tmp_path):
+    """lf_host_rollout.cpp (with lf_host.cpp) on the CPU with -fsanitize=address,undefined: sizes at and past every limit; what
+    reaches a launcher fits its grid, its LDS and the workspace that was asked for."""
+    import subprocess
+    from paper_2602_04789_amd import build
+    exe = build.build_sanitized_host(str(tmp_path), ("lf_host.cpp", "lf_host_rollout.cpp"), "host_rollout_sanitize_driver.cpp",
+                                     "lf_host_rollout_sanitized")
+    env = dict(os.environ, ASAN_OPTIONS="detect_leaks=1:verify_asan_link_order=0", UBSAN_OPTIONS="print_stacktrace=1")
+    res = subprocess.run([exe], stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True, env=env, timeout=120)
+    assert res.returncode == 0 and "ALL OK" in res.stdout, res.stdout[-3000:]
