@@ -541,13 +541,12 @@ def _one_device(at: int, tensors):
             raise ValueError("all tensors must live on the current device")
 
 
-def _new(shape, dtype, like, stream):
+def _new(stream, make, *args, **kw):
     """A tensor for work on `stream`: taken from that stream's memory, so nothing else still uses it there."""
-    torch = _torch or _get_torch()
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=like.device)
-    with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=like.device)
+        return make(*args, **kw)
+    with (_torch or _get_torch()).cuda.stream(stream):
+        return make(*args, **kw)
 
 
 def _rows(t, name: str):
@@ -569,7 +568,7 @@ def _workspace(workspace, need, like, stream, at: int):
     """The caller's scratch, or a new one of need() bytes: a tensor, or None where nothing is needed."""
     if workspace is None:
         n = int(need())
-        return _new(n, (_torch or _get_torch()).uint8, like, stream) if n else None
+        return _new(stream, like.new_empty, n, dtype=(_torch or _get_torch()).uint8) if n else None
     if workspace.get_device() != at or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous tensor on the current device")
     return workspace
@@ -631,12 +630,11 @@ def lf_qk_norm_rope_axes_bwd(X, g, pos, freq, pairs, heads: int, dY, eps: float 
     at, st = _here(stream)
     _one_device(at, (X, g, pos, freq, dY))
     if grads is None:
-        tokens, row = p.tokens, X.stride(0)
-        dg = _new(g.shape, torch.float32, X, stream)
-        if tokens == 1 or row == X.shape[1]:
-            dX = _new(X.shape, torch.bfloat16, X, stream)
+        dg = _new(stream, torch.empty_like, g)
+        if X.is_contiguous():
+            dX = _new(stream, torch.empty_like, X)
         else:
-            dX = _new(tokens * row, torch.bfloat16, X, stream).as_strided(X.shape, X.stride())
+            dX = _new(stream, torch.empty_strided, X.shape, X.stride(), dtype=X.dtype, device=X.device)
     else:
         dX, dg = grads
         if dX.dtype is not torch.bfloat16 or dX.shape != X.shape or dX.stride(1) != 1 or (dX.shape[0] != 1 and dX.stride(0) != X.stride(0)):
@@ -680,9 +678,9 @@ def lf_kvq_read(cache, heads: int, head_dim: int, capacity: int, first: int, tok
     _check_buffer(cache, "cache")
     shape = heads, tokens, d = int(heads), int(tokens), int(head_dim)
     if K is None:
-        K = _new(shape, torch.bfloat16, cache, stream)
+        K = _new(stream, cache.new_empty, shape, dtype=torch.bfloat16)
     if V is None:
-        V = _new(shape, torch.bfloat16, cache, stream)
+        V = _new(stream, cache.new_empty, shape, dtype=torch.bfloat16)
     (ksh, kt, kh), (vsh, vt, vh) = _rows(K, "K"), _rows(V, "V")
     if ksh != shape or vsh != shape:
         raise ValueError("K and V must be [H, tokens, d]")
@@ -710,7 +708,7 @@ def lf_sparse_attn_kvq(Q, cache, capacity: int, kv_len: int, indices, frame_len:
     qsh, qt, qh = _rows(Q, "Q")
     heads, q_len, d = qsh
     if O is None:
-        O = _new(qsh, (_torch or _get_torch()).bfloat16, Q, stream)
+        O = _new(stream, Q.new_empty, qsh)
     osh, ot, oh = _rows(O, "O")
     if osh != qsh:
         raise ValueError("O must be [H, q_len, d]")
@@ -752,7 +750,7 @@ def lf_token_attn_kvq(Q, cache, capacity: int, cached_len: int, K=None, V=None, 
     qsh, qt, qh = _rows(Q, "Q")
     heads, q_len, d = qsh
     if O is None:
-        O = _new(qsh, (_torch or _get_torch()).bfloat16, Q, stream)
+        O = _new(stream, Q.new_empty, qsh)
     osh, ot, oh = _rows(O, "O")
     if osh != qsh:
         raise ValueError("O must be [H, q_len, d]")
