@@ -471,7 +471,9 @@ int lf_kvq_read(const void* cache, size_t cache_bytes, const lf_kvq_shape* cache
  *   workspace  device scratch of >= lf_sparse_attn_kvq_workspace_bytes(), 256-byte aligned (may be NULL where that is 0).
  *              Calls that may overlap must not share it.
  * K and V must be finite, and so must what the cache holds for the listed blocks.
- * Errors: as lf_sparse_attn; LF_ERR_NULL for one of K and V without the other; LF_ERR_WORKSPACE for cache or workspace.
+ * Errors: as lf_sparse_attn; LF_ERR_NULL for one of K and V without the other; LF_ERR_BUDGET also for list_len above 2^30;
+ *   LF_ERR_SHAPE also for heads of O that overlap, more than 2^22 query blocks, heads or head_dim unlike the cache's and a capacity
+ *   below the tokens read; LF_ERR_WORKSPACE for cache or workspace.
  */
 size_t lf_sparse_attn_kvq_workspace_bytes(const lf_shape* shape, int32_t list_len);
 int lf_sparse_attn_kvq(const void* Q, const void* cache, size_t cache_bytes, const lf_kvq_shape* cache_shape,

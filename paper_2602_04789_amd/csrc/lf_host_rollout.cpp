@@ -95,7 +95,7 @@ int check_lists(const lf_shape* s, int32_t list_len, lf_dims* dm) {
   const int rc = lf_derive(&plain, nullptr, dm);
   if (rc != LF_OK) return rc;
   if ((int64_t)dm->H * dm->n_q > kMaxBlocks) return LF_ERR_SHAPE;
-  return list_len < 1 ? LF_ERR_BUDGET : LF_OK;
+  return list_len < 1 || list_len > 1 << 30 ? LF_ERR_BUDGET : LF_OK;      // (a walk along a list steps past its end)
 }
 
 // K or V of all tokens in bfloat16, padded to 256 bytes.

@@ -132,7 +132,7 @@ def test_sparse_attention_over_the_cache_refuses_bad_arguments(lib):
     assert call(Q=None) == call(idx=None) == call(O=None) == call(K=None) == call(V=None) == -1
     assert lib.lf_sparse_attn_kvq(FAKE, FAKE, nbytes, None, None, None, C.byref(_shape()), FAKE, 8, 0.0, FAKE, FAKE, need, None) == -1
     assert lib.lf_sparse_attn_kvq(FAKE, FAKE, nbytes, C.byref(_kvq()), None, None, None, FAKE, 8, 0.0, FAKE, FAKE, need, None) == -1
-    assert call(ll=0) == -3 and call(sc=-1.0) == call(sc=float("nan")) == call(sc=float("inf")) == -2
+    assert call(ll=0) == call(ll=(1 << 30) + 1) == -3 and call(sc=-1.0) == call(sc=float("nan")) == call(sc=float("inf")) == -2
     for kw, code in ((dict(block=32), -2), (dict(head_dim=96), -2), (dict(dtype=1), -4), (dict(heads=11), -2), (dict(q_len=4681), -2),
                      (dict(kv_len=1560), -2), (dict(kv_len=1560 * 25), -2), (dict(k_stride_tok=64), -2), (dict(v_stride_tok=132), -5),
                      (dict(o_stride_head=0), -2), (dict(q_stride_head=4), -5)):
@@ -191,6 +191,31 @@ def test_binding_refuses_wrong_tensors():
                  lambda: lf.lf_sparse_attn_kvq(Y, cache, 8, 8, pos, 4, 64)):
         with pytest.raises(ValueError):
             call()
+
+
+def _parts(H, d, rows, cached, extra=0):
+    """Workgroups that share a head's tokens, from the size of their states."""
+    need = lf.lf_token_attn_kvq_workspace_bytes(H, d, rows, cached, extra)
+    tiles = 1 if rows <= 16 else 2 if rows <= 32 else 4
+    assert need % (H * 16 * tiles * (d + 2) * 4) == 0
+    return need // (H * 16 * tiles * (d + 2) * 4) or 1
+
+
+def test_how_token_attention_is_divided(lib):
+    for rows, cached, extra, H, want in ((1, 1024, 0, 12, 1), (1, 1025, 0, 12, 4), (1, 960, 64, 12, 1), (1, 1024, 1, 12, 4), (32, 1024, 0, 12, 1),
+                                         (33, 512, 0, 12, 1), (33, 513, 0, 12, 2), (64, 131072, 0, 12, 42), (1, 131072, 0, 1, 64),
+                                         (1, 131072, 0, 256, 2), (1, 131072, 0, 257, 1), (1, 0, 1, 600, 1), (1, 0, 0, 3, 1)):
+        assert _parts(H, 128, rows, cached, extra) == want, (rows, cached, extra, H)
+
+
+def test_which_way_list_calls_go(lib):
+    """Few query blocks over a long cache convert what they read; many tiles are worth the cache's rows in bfloat16."""
+    for H, d, n, f, F, length, rows_first in ((12, 128, 1560, 3, 21, 188, True), (12, 64, 1560, 3, 21, 188, True), (12, 128, 64, 1, 400, 40, False),
+                                              (40, 64, 256, 1, 100, 40, False), (1, 128, 256, 2, 260, 1000, False), (12, 128, 1560, 1, 20, 73, False),
+                                              (12, 128, 1560, 1, 20, 180, True), (24, 64, 97, 3, 8, 14, True), (2, 64, 256, 1, 5, 12, False)):
+        need = lf.lf_sparse_attn_kvq_workspace_bytes(H, d, n, 64, f * n, F * n, length)
+        rows = 2 * ((H * F * n * d * 2 + 255) // 256 * 256)
+        assert (need == rows) == rows_first, (H, d, n, f, F, length)
 
 
 def test_host_side_under_address_and_undefined_behaviour_sanitizers(tmp_path):
