@@ -2,15 +2,17 @@
 //
 //   O_x = sum_y softmax_y(q_x . k_y scale) v_y,   y over the tokens of the listed blocks, or over all tokens
 //
-// Few query rows share the cache's bytes, so HBM bounds the call, or with a handful of blocks the chain of one wavefront.
-// Each wavefront has all rows of the block and tiles of 32 tokens of its own: the tiles of a list are dealt out over the four
-// wavefronts of `parts` workgroups, with an online softmax each and nothing shared until the end, so no barrier stands in the loop.
+// Few query rows share the cache's bytes, so HBM bounds the call (one row over 131 076 tokens of 12 x 128: 41 us, 5.2 TB/s of codes and scales),
+// or the chain of a tile where many rows share them (64 rows of 40 x 64 over 32 824 tokens: 43 us, 0.5 PFLOP/s).  A wavefront has up
+// to 32 rows of the block (33 to 64 rows: two wavefronts share them; all in one, with tiles half as long, took 55 us there) and tiles of 64 tokens of
+// its own: the tiles of a list are dealt out over the four wavefronts of `parts` workgroups, with an online softmax each and nothing shared until
+// the end, so no barrier stands in the loop.
 //
 // The products are computed transposed, S^T = K Q^T and O^T = V^T P^T, with v_mfma_f32_16x16x32_bf16.  Their sums run over
 // channels and tokens in any order that both operands agree on.  For S^T a lane takes D/4 neighbouring channels of one token: at d = 128 a
 // whole scaled group, 16 bytes and one scale, straight from memory into the operand, through the conversions that apply the
-// scale.  For O^T a lane takes the tokens whose scores the first product left it (4 kg + {0..3} of the two halves of the tile),
-// so P stays in its registers; V goes through LDS as bfloat16 rows and comes back by the transposing read.  The bytes of
+// scale.  For O^T a lane takes the tokens whose scores the first product left it (4 kg + {0..3} of each 16 tokens of the tile),
+// so P stays in its registers; V goes through LDS as bfloat16 rows, half a tile at a time, and comes back by the transposing read.  The bytes of
 // the next tile are requested as soon as those of the present one are converted.
 //
 // Softmax is float32 in the exp2 domain, P = exp2(s c - m), against a reference m per row that moves only when a tile's sum of P is large:
@@ -387,7 +389,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void lf_kvq_attn_kernel(KvqAttnArgs
   }
 }
 
-// Joins the parts of a row: a workgroup each, its wavefronts taking every fourth part, lane p holding part p's weight.
+// Joins the parts of a row: a workgroup each, its wavefronts taking every fourth part, lane p holding part p's weight (12 rows of 42 parts: 4 us, two
+// loads one after the other and a launch; a wavefront a row, one part after the other: 13).
 template <int D>
 __global__ __launch_bounds__(64 * kWaves) void lf_kvq_join_kernel(KvqAttnArgs a, int rows_max, int tile_rows) {
   constexpr int W = D / 64;       // channels of a lane

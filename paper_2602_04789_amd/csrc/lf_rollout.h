@@ -73,7 +73,7 @@ struct lf_kvq_call {
   int parts;                   // workgroups that share a query block's list
   void* workspace;
 };
-// 16 query rows each that a wavefront holds.
+// Tiles of 16 query rows of a block; a wavefront holds one or two of them, so two wavefronts share a block of four.
 inline int lf_kvq_tiles(int rows) { return rows <= 16 ? 1 : rows <= 32 ? 2 : 4; }
 #define LF_KVQ_MAX_PARTS 64     // a lane of the joining wavefront each
 // Into how many workgroups of four wavefronts the list of a query block is divided: until every compute unit has two, as long as each
