@@ -273,7 +273,8 @@ __global__ __launch_bounds__(512) void lf_rope_axes_bwd_kernel(AxesArgs a) {
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
       const int h = hp + i * a.hpt;
-      const float inv = 1.0f / sqrtf(ss[i] / n + a.eps);
+      // threads without a token add nothing to dg: with eps = 0 their 1 / sqrt(0) times their zeros would be NaN
+      const float inv = there ? 1.0f / sqrtf(ss[i] / n + a.eps) : 0.0f;
       const float mean = ux[i] * inv / n;
       float x[8], r[8];
       unpack8(xr[i], x);
