@@ -541,6 +541,24 @@ def _one_device(at: int, tensors):
             raise ValueError("all tensors must live on the current device")
 
 
+def _int32(*values):
+    """Sizes and places for int32 fields of the C structures, which would drop the bits above."""
+    values = tuple(map(int, values))
+    for v in values:        # (two thirds of the time that min() and max() take)
+        if not -0x80000000 <= v <= 0x7FFFFFFF:
+            raise ValueError("a size or place does not fit 32 bits")
+    return values
+
+
+def _size_of(query, make, *values) -> int:
+    """What a size query of the library says of the structure that `make` builds from whole numbers, 0 where one does not fit."""
+    try:
+        shape, *more = make(*_int32(*values))
+    except ValueError:
+        return 0
+    return int(query(C.byref(shape), *more))
+
+
 def _new(stream, make, *args, **kw):
     """A tensor for work on `stream`: taken from that stream's memory, so nothing else still uses it there."""
     if stream is None:
@@ -578,8 +596,11 @@ def _bytes_of(t):
     return (0, 0) if t is None else (t.data_ptr(), t.numel() * t.element_size())
 
 
-def _axes_shape(X, g, pos, freq, pairs, heads, rows, eps, across_heads, pairing) -> lf_axes_shape:
+def _axes_shape(X, g, pos, freq, pairs, heads, out, eps, across_heads, pairing) -> lf_axes_shape:
     torch = _torch or _get_torch()
+    if len(pairs) != 3:
+        raise ValueError("pairs must be three numbers")
+    heads, pairing, *pairs = _int32(heads, pairing, *pairs)
     if not X.is_cuda or X.dtype is not torch.bfloat16:
         raise ValueError("X must be a bfloat16 GPU tensor")
     if g.dtype is not torch.float32 or not g.is_contiguous():
@@ -588,14 +609,13 @@ def _axes_shape(X, g, pos, freq, pairs, heads, rows, eps, across_heads, pairing)
         raise ValueError("pos must be contiguous int32 [L, 3]")
     if freq.dtype is not torch.float64 or not freq.is_contiguous():
         raise ValueError("freq must be contiguous float64 [d / 2]")
-    (yheads, tokens, d), yt, yh = rows
-    heads = int(heads)
+    (yheads, tokens, d), yt, yh = _rows(*out)
     xs, xsh = X.stride(), X.shape
     if len(xs) != 2 or xs[1] != 1 or xsh[0] != tokens or yheads != heads:
         raise ValueError("X must be [L, >= H * d] with contiguous channels, Y and dY [H, L, d]")
-    if xsh[1] < heads * d or g.numel() != heads * d or pos.shape != (tokens, 3) or freq.numel() != d // 2 or len(pairs) != 3:
+    if xsh[1] < heads * d or g.numel() != heads * d or pos.shape != (tokens, 3) or freq.numel() != d // 2:
         raise ValueError("shapes of X, g, pos, freq or pairs do not fit")
-    return lf_axes_shape(heads, d, tokens, 1 if across_heads else 0, int(pairing), (int(pairs[0]), int(pairs[1]), int(pairs[2])), float(eps), 0,
+    return lf_axes_shape(heads, d, tokens, 1 if across_heads else 0, pairing, tuple(pairs), float(eps), 0,
                          xs[0] if tokens != 1 else heads * d, yt, yh)
 
 
@@ -604,7 +624,7 @@ def lf_qk_norm_rope_axes(X, g, pos, freq, pairs, heads: int, Y, eps: float = 1e-
     """RMSNorm and rotary positions over three axes of the token-major activation X [L, >= H*d] (bfloat16) into the head-major
     tensor Y [H, L, d] (bfloat16; may be a view into Q or into the K cache).  ``pos`` int32 [L, 3] (time, height, width),
     ``freq`` float64 [d/2] in radians per position, ``pairs`` how many channel pairs each axis has."""
-    p = _axes_shape(X, g, pos, freq, pairs, heads, _rows(Y, "Y"), eps, across_heads, pairing)
+    p = _axes_shape(X, g, pos, freq, pairs, heads, (Y, "Y"), eps, across_heads, pairing)
     at, st = _here(stream)
     _one_device(at, (X, g, pos, freq, Y))
     rc = (_lib or load()).lf_qk_norm_rope_axes(X.data_ptr(), g.data_ptr(), pos.data_ptr(), freq.data_ptr(), C.byref(p),
@@ -615,9 +635,8 @@ def lf_qk_norm_rope_axes(X, g, pos, freq, pairs, heads: int, Y, eps: float = 1e-
 
 
 def lf_qk_norm_rope_axes_bwd_workspace_bytes(heads: int, head_dim: int, tokens: int) -> int:
-    H, d, L = int(heads), int(head_dim), int(tokens)
-    p = lf_axes_shape(H, d, L, 0, 0, (d // 2, 0, 0), 0.0, 0, H * d, d, L * d)
-    return int(load().lf_qk_norm_rope_axes_bwd_workspace_bytes(C.byref(p)))
+    return _size_of(load().lf_qk_norm_rope_axes_bwd_workspace_bytes,
+                    lambda H, d, L: (lf_axes_shape(H, d, L, 0, 0, (d // 2, 0, 0), 0.0, 0, H * d, d, L * d),), heads, head_dim, tokens)
 
 
 def lf_qk_norm_rope_axes_bwd(X, g, pos, freq, pairs, heads: int, dY, eps: float = 1e-6, across_heads: bool = False,
@@ -626,7 +645,7 @@ def lf_qk_norm_rope_axes_bwd(X, g, pos, freq, pairs, heads: int, dY, eps: float 
     shape and row stride of X, of which the first H*d channels are written, dg float32 [H*d] (``grads``: two such tensors to
     write into instead of new ones)."""
     torch = _torch or _get_torch()
-    p = _axes_shape(X, g, pos, freq, pairs, heads, _rows(dY, "dY"), eps, across_heads, pairing)
+    p = _axes_shape(X, g, pos, freq, pairs, heads, (dY, "dY"), eps, across_heads, pairing)
     at, st = _here(stream)
     _one_device(at, (X, g, pos, freq, dY))
     if grads is None:
@@ -653,20 +672,21 @@ def lf_qk_norm_rope_axes_bwd(X, g, pos, freq, pairs, heads: int, dY, eps: float 
 
 def lf_kvq_bytes(heads: int, head_dim: int, capacity: int) -> int:
     """Bytes of a 4-bit cache for `capacity` tokens (0 on bad input)."""
-    return int(load().lf_kvq_bytes(C.byref(lf_kvq_shape(int(heads), int(head_dim), int(capacity), 0))))
+    return _size_of(load().lf_kvq_bytes, lambda *sizes: (lf_kvq_shape(*sizes),), heads, head_dim, capacity)
 
 
 def lf_kvq_append(K, V, cache, capacity: int, first: int, stream=None):
     """Write the tokens [first, first + L) of the 4-bit cache from K and V [H, L, d] (bfloat16); returns ``cache`` (a uint8
     device tensor of >= lf_kvq_bytes())."""
+    capacity, first = _int32(capacity, first)
     (sh, kt, kh), (vsh, vt, vh) = _rows(K, "K"), _rows(V, "V")
     _check_buffer(cache, "cache")
     if sh != vsh:
         raise ValueError("K and V must have one shape")
     at, st = _here(stream)
     _one_device(at, (K, V, cache))
-    rc = (_lib or load()).lf_kvq_append(K.data_ptr(), V.data_ptr(), C.byref(lf_kvq_shape(sh[0], sh[2], int(capacity))),
-                                        C.byref(lf_kvq_rows(int(first), sh[1], kt, kh, vt, vh)), cache.data_ptr(), cache.numel(), st)
+    rc = (_lib or load()).lf_kvq_append(K.data_ptr(), V.data_ptr(), C.byref(lf_kvq_shape(sh[0], sh[2], capacity)),
+                                        C.byref(lf_kvq_rows(first, sh[1], kt, kh, vt, vh)), cache.data_ptr(), cache.numel(), st)
     if rc != LF_OK:
         raise LfError(rc, "lf_kvq_append")
     return cache
@@ -675,8 +695,9 @@ def lf_kvq_append(K, V, cache, capacity: int, first: int, stream=None):
 def lf_kvq_read(cache, heads: int, head_dim: int, capacity: int, first: int, tokens: int, K=None, V=None, stream=None):
     """The values that tokens [first, first + tokens) of the 4-bit cache stand for: (K, V), bfloat16 [H, tokens, d]."""
     torch = _torch or _get_torch()
+    heads, d, capacity, first, tokens = _int32(heads, head_dim, capacity, first, tokens)
     _check_buffer(cache, "cache")
-    shape = heads, tokens, d = int(heads), int(tokens), int(head_dim)
+    shape = heads, tokens, d
     if K is None:
         K = _new(stream, cache.new_empty, shape, dtype=torch.bfloat16)
     if V is None:
@@ -686,8 +707,8 @@ def lf_kvq_read(cache, heads: int, head_dim: int, capacity: int, first: int, tok
         raise ValueError("K and V must be [H, tokens, d]")
     at, st = _here(stream)
     _one_device(at, (cache, K, V))
-    rc = (_lib or load()).lf_kvq_read(cache.data_ptr(), cache.numel(), C.byref(lf_kvq_shape(heads, d, int(capacity))),
-                                      C.byref(lf_kvq_rows(int(first), tokens, kt, kh, vt, vh)), K.data_ptr(), V.data_ptr(), st)
+    rc = (_lib or load()).lf_kvq_read(cache.data_ptr(), cache.numel(), C.byref(lf_kvq_shape(heads, d, capacity)),
+                                      C.byref(lf_kvq_rows(first, tokens, kt, kh, vt, vh)), K.data_ptr(), V.data_ptr(), st)
     if rc != LF_OK:
         raise LfError(rc, "lf_kvq_read")
     return K, V
@@ -695,15 +716,16 @@ def lf_kvq_read(cache, heads: int, head_dim: int, capacity: int, first: int, tok
 
 def lf_sparse_attn_kvq_workspace_bytes(heads: int, head_dim: int, frame_len: int, block: int, q_len: int, kv_len: int,
                                        list_len: int) -> int:
-    d = int(head_dim)
-    sh = lf_shape(int(heads), d, int(frame_len), int(block), int(q_len), int(kv_len), LF_BF16, 0, d, 0, d, 0, d, 0, d, 0)
-    return int(load().lf_sparse_attn_kvq_workspace_bytes(C.byref(sh), int(list_len)))
+    return _size_of(load().lf_sparse_attn_kvq_workspace_bytes,
+                    lambda H, d, n, b, q, kv, length: (lf_shape(H, d, n, b, q, kv, LF_BF16, 0, d, 0, d, 0, d, 0, d, 0), length),
+                    heads, head_dim, frame_len, block, q_len, kv_len, list_len)
 
 
 def lf_sparse_attn_kvq(Q, cache, capacity: int, kv_len: int, indices, frame_len: int, block: int, K=None, V=None,
                        softmax_scale: float = 0.0, O=None, workspace=None, stream=None):
     """Blockwise sparse attention over the 4-bit cache; returns O (bfloat16 [H, q_len, d], device).  With ``K`` and ``V`` [H, q_len,
     d] the current chunk's tokens, the last q_len of kv_len, are read from them in bfloat16, without them from the cache."""
+    capacity, kv_len, frame_len, block = _int32(capacity, kv_len, frame_len, block)
     _check_buffer(cache, "cache")
     qsh, qt, qh = _rows(Q, "Q")
     heads, q_len, d = qsh
@@ -724,12 +746,12 @@ def lf_sparse_attn_kvq(Q, cache, capacity: int, kv_len: int, indices, frame_len:
         raise ValueError("K and V go together")
     else:
         _one_device(at, (Q, cache, indices, O))
-    sh = lf_shape(heads, d, int(frame_len), int(block), q_len, int(kv_len), LF_BF16, 0, qt, qh, kt, kh, vt, vh, ot, oh)
-    _check_lists(indices, sh, sh.frame_len)
-    length = indices.shape[2]
+    sh = lf_shape(heads, d, frame_len, block, q_len, kv_len, LF_BF16, 0, qt, qh, kt, kh, vt, vh, ot, oh)
+    _check_lists(indices, sh, frame_len)
+    length, = _int32(indices.shape[2])
     lib = _lib or load()
     ws = _workspace(workspace, lambda: lib.lf_sparse_attn_kvq_workspace_bytes(C.byref(sh), length), Q, stream, at)
-    rc = lib.lf_sparse_attn_kvq(Q.data_ptr(), cache.data_ptr(), cache.numel(), C.byref(lf_kvq_shape(heads, d, int(capacity))),
+    rc = lib.lf_sparse_attn_kvq(Q.data_ptr(), cache.data_ptr(), cache.numel(), C.byref(lf_kvq_shape(heads, d, capacity)),
                                 k_ptr, v_ptr, C.byref(sh), indices.data_ptr(), length, float(softmax_scale), O.data_ptr(), *_bytes_of(ws), st)
     if rc != LF_OK:
         raise LfError(rc, "lf_sparse_attn_kvq")
@@ -737,15 +759,16 @@ def lf_sparse_attn_kvq(Q, cache, capacity: int, kv_len: int, indices, frame_len:
 
 
 def lf_token_attn_kvq_workspace_bytes(heads: int, head_dim: int, q_len: int, cached_len: int, extra_len: int) -> int:
-    d = int(head_dim)
-    sh = lf_token_shape(int(heads), d, int(q_len), int(cached_len), int(extra_len), 0, d, 0, d, 0, d, 0, d, 0)
-    return int(load().lf_token_attn_kvq_workspace_bytes(C.byref(sh)))
+    return _size_of(load().lf_token_attn_kvq_workspace_bytes,
+                    lambda H, d, q, held, extra: (lf_token_shape(H, d, q, held, extra, 0, d, 0, d, 0, d, 0, d, 0),),
+                    heads, head_dim, q_len, cached_len, extra_len)
 
 
 def lf_token_attn_kvq(Q, cache, capacity: int, cached_len: int, K=None, V=None, softmax_scale: float = 0.0, O=None,
                       workspace=None, stream=None):
     """Attention of up to 64 query rows [H, q_len, d] over the first ``cached_len`` tokens of the 4-bit cache and the tokens of ``K``
     and ``V`` [H, extra, d] (bfloat16, optional) behind them; returns O (bfloat16 [H, q_len, d], device)."""
+    capacity, cached_len = _int32(capacity, cached_len)
     _check_buffer(cache, "cache")
     qsh, qt, qh = _rows(Q, "Q")
     heads, q_len, d = qsh
@@ -767,10 +790,10 @@ def lf_token_attn_kvq(Q, cache, capacity: int, cached_len: int, K=None, V=None, 
         raise ValueError("K and V go together")
     else:
         _one_device(at, (Q, cache, O))
-    sh = lf_token_shape(heads, d, q_len, int(cached_len), extra, 0, qt, qh, kt, kh, vt, vh, ot, oh)
+    sh = lf_token_shape(heads, d, q_len, cached_len, extra, 0, qt, qh, kt, kh, vt, vh, ot, oh)
     lib = _lib or load()
     ws = _workspace(workspace, lambda: lib.lf_token_attn_kvq_workspace_bytes(C.byref(sh)), Q, stream, at)
-    rc = lib.lf_token_attn_kvq(Q.data_ptr(), cache.data_ptr(), cache.numel(), C.byref(lf_kvq_shape(heads, d, int(capacity))),
+    rc = lib.lf_token_attn_kvq(Q.data_ptr(), cache.data_ptr(), cache.numel(), C.byref(lf_kvq_shape(heads, d, capacity)),
                                k_ptr, v_ptr, C.byref(sh), float(softmax_scale), O.data_ptr(), *_bytes_of(ws), st)
     if rc != LF_OK:
         raise LfError(rc, "lf_token_attn_kvq")
