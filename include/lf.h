@@ -400,8 +400,8 @@ int lf_qk_norm_rope(const void* X, const float* g, const float* cos_table, const
  *   dg       device, float32 [H*d], written.
  *   workspace  device scratch of >= lf_qk_norm_rope_axes_bwd_workspace_bytes(), 256-byte aligned.
  *   X, Y, dY, dX, g 16-byte aligned, freq 8, pos and dg 4; strides multiples of 8.  Y must not overlap X.
- * Errors: LF_ERR_NULL, LF_ERR_SHAPE (as lf_qk_norm_rope; H*d above 16 384; pairs negative or not adding up to d/2; more
- *   than 2^32 threads' worth of tokens, some 10^11 values), LF_ERR_ALIGN, LF_ERR_WORKSPACE, LF_ERR_HIP.
+ * Errors: LF_ERR_NULL, LF_ERR_SHAPE (as lf_qk_norm_rope; H*d above 16 384; pairs negative or not adding up to d/2; heads of
+ *   Y that share an element; more than 2^32 threads' worth of tokens, some 10^11 values), LF_ERR_ALIGN, LF_ERR_WORKSPACE, LF_ERR_HIP.
  */
 typedef struct {
   int32_t heads;        /* H */
@@ -436,7 +436,7 @@ int lf_qk_norm_rope_axes_bwd(const void* X, const float* g, const int32_t* pos, 
  *   lf_kvq_read     the reverse: K and V are written with the values that the cache holds.
  *   tokens = 0 enqueues nothing.
  * Errors: LF_ERR_NULL; LF_ERR_SHAPE (head_dim not 64 or 128, heads not in 1 .. 32 767, capacity not in 1 .. 2^24, tokens outside
- *   the cache, a row stride below d); LF_ERR_ALIGN; LF_ERR_WORKSPACE (cache missing or too small); LF_ERR_HIP.
+ *   the cache, a row stride below d, heads of what lf_kvq_read writes that share an element); LF_ERR_ALIGN; LF_ERR_WORKSPACE (cache missing or too small); LF_ERR_HIP.
  */
 typedef struct {
   int32_t heads;        /* H */
@@ -472,7 +472,7 @@ int lf_kvq_read(const void* cache, size_t cache_bytes, const lf_kvq_shape* cache
  *              Calls that may overlap must not share it.
  * K and V must be finite, and so must what the cache holds for the listed blocks.
  * Errors: as lf_sparse_attn; LF_ERR_NULL for one of K and V without the other; LF_ERR_BUDGET also for list_len above 2^30;
- *   LF_ERR_SHAPE also for heads of O that overlap, more than 2^22 query blocks, heads or head_dim unlike the cache's and a capacity
+ *   LF_ERR_SHAPE also for heads of O that share an element, more than 2^22 query blocks, heads or head_dim unlike the cache's and a capacity
  *   below the tokens read; LF_ERR_WORKSPACE for cache or workspace.
  */
 size_t lf_sparse_attn_kvq_workspace_bytes(const lf_shape* shape, int32_t list_len);
@@ -488,7 +488,7 @@ int lf_sparse_attn_kvq(const void* Q, const void* cache, size_t cache_bytes, con
  * The long axis is divided among workgroups and joined in a fixed order.  Without any token the rows are zeros.
  * workspace and the rest as lf_sparse_attn_kvq.
  * Errors: LF_ERR_NULL; LF_ERR_SHAPE (q_len not in 1 .. 64, lengths negative or above 2^24, cached_len above the capacity, heads or head_dim
- *   unlike the cache's); LF_ERR_ALIGN; LF_ERR_WORKSPACE; LF_ERR_HIP.
+ *   unlike the cache's, heads of O that share an element); LF_ERR_ALIGN; LF_ERR_WORKSPACE; LF_ERR_HIP.
  */
 typedef struct {
   int32_t heads, head_dim;

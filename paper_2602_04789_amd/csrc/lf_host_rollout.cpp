@@ -17,8 +17,19 @@ int check_strides(const int64_t* tok_head, int n, int64_t width) {
   return LF_OK;
 }
 
-// Heads of a tensor that is written must lie apart.
-bool heads_overlap(int heads, int64_t stride_head, int d) { return heads > 1 && stride_head < d; }
+// Whether rows of two heads share an element, in a tensor that is written: head h's token t takes [h stride_head + t stride_tok, .. + d).  One
+// head's tokens lie apart (stride_tok >= d).  Layouts with one axis inside a step of the other are seen at once.
+bool heads_overlap(int heads, int64_t stride_head, int tokens, int64_t stride_tok, int d) {
+  if (heads < 2) return false;
+  if (stride_head < d) return true;
+  if (tokens < 2 || (stride_head - d) / stride_tok >= tokens - 1 || (stride_tok - d) / stride_head >= heads - 1) return false;
+  for (int h = 1; h < heads; ++h) {             // heads h apart, and the tokens on both sides of where the later one begins
+    const __int128 off = (__int128)h * stride_head, t = off / stride_tok, past = off - t * stride_tok;
+    if (t < tokens && past < d) return true;
+    if (t + 1 < tokens && stride_tok - past < d) return true;
+  }
+  return false;
+}
 
 bool scale_ok(float s) { return s >= 0.0f && !isinf(s); }
 float scale_or_default(float s, int d) { return s > 0.0f ? s : 1.0f / sqrtf((float)d); }
@@ -110,7 +121,7 @@ extern "C" int lf_qk_norm_rope_axes(const void* X, const float* g, const int32_t
   if (!X || !g || !pos || !freq || !p || !Y) return LF_ERR_NULL;
   const int rc = check_axes(p);
   if (rc != LF_OK) return rc;
-  if (heads_overlap(p->heads, p->y_stride_head, p->head_dim)) return LF_ERR_SHAPE;
+  if (heads_overlap(p->heads, p->y_stride_head, p->tokens, p->y_stride_tok, p->head_dim)) return LF_ERR_SHAPE;
   if (axes_misaligned(X, g, pos, freq) || misaligned(Y, 16)) return LF_ERR_ALIGN;
   return lf_launch_rope_axes(X, g, pos, freq, p, Y, stream);
 }
@@ -153,7 +164,9 @@ extern "C" int lf_kvq_read(const void* cache, size_t cache_bytes, const lf_kvq_s
   int rc = check_cache(s);
   if (rc != LF_OK) return rc;
   if ((rc = check_rows(s, r)) != LF_OK) return rc;
-  if (heads_overlap(s->heads, r->k_stride_head, s->head_dim) || heads_overlap(s->heads, r->v_stride_head, s->head_dim)) return LF_ERR_SHAPE;
+  if (heads_overlap(s->heads, r->k_stride_head, r->tokens, r->k_stride_tok, s->head_dim) ||
+      heads_overlap(s->heads, r->v_stride_head, r->tokens, r->v_stride_tok, s->head_dim))
+    return LF_ERR_SHAPE;
   if (!cache || cache_bytes < lf_kvq_bytes(s)) return LF_ERR_WORKSPACE;
   if (misaligned(K, 16) || misaligned(V, 16) || misaligned(cache, 256)) return LF_ERR_ALIGN;
   return r->tokens == 0 ? LF_OK : lf_launch_kvq_read((const uint8_t*)cache, s, r, K, V, stream);
@@ -174,7 +187,7 @@ extern "C" int lf_sparse_attn_kvq(const void* Q, const void* cache, size_t cache
   lf_dims dm;
   int rc = check_lists(s, list_len, &dm);
   if (rc != LF_OK) return rc;
-  if (heads_overlap(s->heads, s->o_stride_head, s->head_dim)) return LF_ERR_SHAPE;
+  if (heads_overlap(s->heads, s->o_stride_head, s->q_len, s->o_stride_tok, s->head_dim)) return LF_ERR_SHAPE;
   if (K) {
     const int64_t st[4] = {s->k_stride_tok, s->k_stride_head, s->v_stride_tok, s->v_stride_head};
     if ((rc = check_strides(st, 2, s->head_dim)) != LF_OK) return rc;
@@ -228,7 +241,7 @@ extern "C" int lf_token_attn_kvq(const void* Q, const void* cache, size_t cache_
   int rc = check_token(s);
   if (rc != LF_OK) return rc;
   if (s->extra_len > 0 && (!K || !V)) return LF_ERR_NULL;
-  if (heads_overlap(s->heads, s->o_stride_head, s->head_dim)) return LF_ERR_SHAPE;
+  if (heads_overlap(s->heads, s->o_stride_head, s->q_len, s->o_stride_tok, s->head_dim)) return LF_ERR_SHAPE;
   if ((rc = check_call(Q, cache, cache_bytes, cs, K, V, softmax_scale, O, s->heads, s->head_dim, s->cached_len)) != LF_OK) return rc;
   const size_t need = lf_token_attn_kvq_workspace_bytes(s);
   if (need > 0 && (!workspace || workspace_bytes < need)) return LF_ERR_WORKSPACE;

@@ -1,0 +1,74 @@
+"""Layouts of what the rollout's calls write: rows of two heads that share an element are refused (they would be written by two
+workgroups), every other layout is taken as far as the next check, here a pointer that is refused.  No GPU, nothing is enqueued."""
+import ctypes as C
+import os
+import random
+
+import pytest
+
+from paper_2602_04789_amd import lf
+
+FAKE = 0x10000
+SHAPE, ALIGN, WORKSPACE = -2, -5, -6
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if not os.path.exists(lf.library_path()):
+        from paper_2602_04789_amd import build
+        build.build()
+    return lf.load()
+
+
+def _overlap(heads, stride_head, tokens, stride_tok, d):
+    """By laying the rows out."""
+    seen = set()
+    for h in range(heads):
+        for t in range(tokens):
+            for at in range(h * stride_head + t * stride_tok, h * stride_head + t * stride_tok + d, 8):
+                if at in seen:
+                    return True
+                seen.add(at)
+    return False
+
+
+def _calls(lib, heads, stride_head, tokens, stride_tok, d):
+    """The status of each call that writes such a tensor, and the one that it has where the layout is fine."""
+    ap = lf.lf_axes_shape(heads, d, tokens, 0, 0, (d // 2, 0, 0), 1e-6, 0, heads * d, stride_tok, stride_head)
+    yield lib.lf_qk_norm_rope_axes(FAKE, FAKE, FAKE, FAKE, C.byref(ap), FAKE + 2, None), ALIGN
+    cs = lf.lf_kvq_shape(heads, d, 5000, 0)
+    ok = (d, d * tokens)
+    for k, v in (((stride_tok, stride_head), ok), (ok, (stride_tok, stride_head))):
+        rows = lf.lf_kvq_rows(0, tokens, *k, *v)
+        yield lib.lf_kvq_read(None, 0, C.byref(cs), C.byref(rows), FAKE, FAKE, None), WORKSPACE
+    sh = lf.lf_shape(heads, d, tokens, 64, tokens, tokens, 0, 0, *ok, *ok, *ok, stride_tok, stride_head)
+    yield lib.lf_sparse_attn_kvq(FAKE, None, 0, C.byref(cs), None, None, C.byref(sh), FAKE, 1, 0.0, FAKE, None, 0, None), WORKSPACE
+    if tokens <= 64:
+        ts = lf.lf_token_shape(heads, d, tokens, 5, 0, 0, *ok, *ok, *ok, stride_tok, stride_head)
+        yield lib.lf_token_attn_kvq(FAKE, None, 0, C.byref(cs), None, None, C.byref(ts), 0.0, FAKE, None, 0, None), WORKSPACE
+
+
+def test_rows_that_share_elements_are_refused(lib):
+    rng = random.Random(0)
+    both = [0, 0]
+    for _ in range(3000):
+        d, heads, tokens = rng.choice([64, 128]), rng.randint(1, 6), rng.randint(1, 6)
+        stride_tok, stride_head = d + 8 * rng.randint(0, 5 * d // 8), 8 * rng.randint(0, 6 * d // 8)
+        bad = _overlap(heads, stride_head, tokens, stride_tok, d)
+        both[bad] += 1
+        for status, fine in _calls(lib, heads, stride_head, tokens, stride_tok, d):
+            assert status == (SHAPE if bad else fine), (heads, stride_head, tokens, stride_tok, d)
+    assert min(both) > 500
+
+
+@pytest.mark.parametrize("heads,stride_head,tokens,stride_tok,d,bad", [
+    (2, 64, 2, 64, 64, True),                       # head 1's first token is head 0's second
+    (12, 128 * 4679, 4680, 128, 128, True), (12, 128 * 4680, 4680, 128, 128, False),        # a head begins on the last token of the one before
+    (12, 128, 4680, 1536, 128, False), (13, 128, 4680, 1536, 128, True),                    # token-major rows
+    (2, 3 * 64, 100, 2 * 64, 64, False),            # heads between each other's tokens
+    (256, 64, 1, 64, 64, False), (256, 56, 1, 64, 64, True),
+    (3, (2 ** 63 - 1) // 8 * 8, 3, (2 ** 63 - 1) // 8 * 8, 64, True), (2, 2 ** 62, 4, 2 ** 60, 64, False), (2, 2 ** 62, 5, 2 ** 60, 64, True),
+    (128, 2 ** 62, 4, 2 ** 60, 64, False)])
+def test_named_layouts(lib, heads, stride_head, tokens, stride_tok, d, bad):
+    for k, (status, fine) in enumerate(_calls(lib, heads, stride_head, tokens, stride_tok, d)):
+        assert status == (SHAPE if bad else fine), k
