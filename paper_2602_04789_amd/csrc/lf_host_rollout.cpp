@@ -240,7 +240,8 @@ extern "C" int lf_token_attn_kvq(const void* Q, const void* cache, size_t cache_
   if (!Q || !cs || !s || !O) return LF_ERR_NULL;
   int rc = check_token(s);
   if (rc != LF_OK) return rc;
-  if (s->extra_len > 0 && (!K || !V)) return LF_ERR_NULL;
+  if (s->extra_len == 0) K = V = nullptr;
+  else if (!K || !V) return LF_ERR_NULL;
   if (heads_overlap(s->heads, s->o_stride_head, s->q_len, s->o_stride_tok, s->head_dim)) return LF_ERR_SHAPE;
   if ((rc = check_call(Q, cache, cache_bytes, cs, K, V, softmax_scale, O, s->heads, s->head_dim, s->cached_len)) != LF_OK) return rc;
   const size_t need = lf_token_attn_kvq_workspace_bytes(s);

@@ -19,3 +19,12 @@ def test_places_that_do_not_fit_are_refused_and_nothing_is_written(gpu):  # noqa
             call()
     torch.cuda.synchronize()
     assert torch.equal(cache, before)
+
+
+def test_rows_behind_the_cache_at_an_odd_address_without_a_row(gpu):  # noqa: F811
+    torch, lf = gpu
+    H, d, T = 2, 64, 70
+    dev, host = _cache(gpu, H, T, d, _rand(torch, 1, H, T, d), _rand(torch, 2, H, T, d))
+    Q, none = _rand(torch, 3, H, 2, d).cuda(), torch.zeros(9 * d, dtype=torch.bfloat16, device="cuda")[3:].as_strided((H, 0, d), (d, d, 1))
+    want = lf.lf_token_attn_kvq(Q, dev, T, T)
+    assert torch.equal(lf.lf_token_attn_kvq(Q, dev, T, T, K=none, V=none), want)

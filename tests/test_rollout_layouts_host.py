@@ -72,3 +72,13 @@ def test_rows_that_share_elements_are_refused(lib):
 def test_named_layouts(lib, heads, stride_head, tokens, stride_tok, d, bad):
     for k, (status, fine) in enumerate(_calls(lib, heads, stride_head, tokens, stride_tok, d)):
         assert status == (SHAPE if bad else fine), k
+
+
+def test_rows_behind_the_cache_are_not_looked_at_where_there_are_none(lib):
+    """extra_len = 0: K and V may be anything, a slice without a row at an odd address among it; the next check is the workspace's."""
+    cs = lf.lf_kvq_shape(12, 128, 32760, 0)
+    nbytes = lf.lf_kvq_bytes(12, 128, 32760)
+    for extra, ptr, status in ((0, FAKE + 2, WORKSPACE), (0, None, WORKSPACE), (1, FAKE + 2, ALIGN), (1, FAKE, WORKSPACE), (1, None, -1)):
+        for K, V in ((ptr, FAKE), (FAKE, ptr), (ptr, ptr)):
+            ts = lf.lf_token_shape(12, 128, 1, 32760, extra, 0, 128, 128, 128, 128, 128, 128, 128, 128)
+            assert lib.lf_token_attn_kvq(FAKE, FAKE, nbytes, C.byref(cs), K, V, C.byref(ts), 0.0, FAKE, None, 0, None) == status, (extra, K, V)
