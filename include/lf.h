@@ -469,7 +469,10 @@ int lf_kvq_read(const void* cache, size_t cache_bytes, const lf_kvq_shape* cache
  *              duplicates count twice, rows without a valid id are zeros).
  *   cache, cache_shape   heads and head_dim as in `shape`, capacity at least the tokens read from it.
  *   workspace  device scratch of >= lf_sparse_attn_kvq_workspace_bytes(), 256-byte aligned (may be NULL where that is 0).
- *              Calls that may overlap must not share it.
+ *              Calls that may overlap must not share it.  The size is this call's alone and can fall as kv_len or list_len changes: calls
+ *              with many tiles first write K and V of all kv_len tokens in bfloat16 (two parts of H * kv_len * d * 2 bytes, padded to 256:
+ *              3.8 times the cache), calls with fewer need at most 512 * 64 * (d + 2) * 4 bytes, or none.  One buffer for the chunks of a
+ *              rollout has the largest of their sizes, which need not be the last chunk's.
  * K and V must be finite, and so must what the cache holds for the listed blocks.
  * Errors: as lf_sparse_attn; LF_ERR_NULL for one of K and V without the other; LF_ERR_BUDGET also for list_len above 2^30;
  *   LF_ERR_SHAPE also for heads of O that share an element, more than 2^22 query blocks, heads or head_dim unlike the cache's and a capacity

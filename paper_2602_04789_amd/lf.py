@@ -716,6 +716,7 @@ def lf_kvq_read(cache, heads: int, head_dim: int, capacity: int, first: int, tok
 
 def lf_sparse_attn_kvq_workspace_bytes(heads: int, head_dim: int, frame_len: int, block: int, q_len: int, kv_len: int,
                                        list_len: int) -> int:
+    """Scratch of one call (0 on bad input too).  It can be less for a longer cache: a buffer for several calls has the largest of their sizes."""
     return _size_of(load().lf_sparse_attn_kvq_workspace_bytes,
                     lambda H, d, n, b, q, kv, length: (lf_shape(H, d, n, b, q, kv, LF_BF16, 0, d, 0, d, 0, d, 0, d, 0), length),
                     heads, head_dim, frame_len, block, q_len, kv_len, list_len)
