@@ -82,3 +82,14 @@ def test_rows_behind_the_cache_are_not_looked_at_where_there_are_none(lib):
         for K, V in ((ptr, FAKE), (FAKE, ptr), (ptr, ptr)):
             ts = lf.lf_token_shape(12, 128, 1, 32760, extra, 0, 128, 128, 128, 128, 128, 128, 128, 128)
             assert lib.lf_token_attn_kvq(FAKE, FAKE, nbytes, C.byref(cs), K, V, C.byref(ts), 0.0, FAKE, None, 0, None) == status, (extra, K, V)
+
+
+def test_range_of_eps(lib):
+    """What the producer and its gradients take for eps: from 0 on, nothing that is not finite."""
+    for eps, taken in ((0.0, True), (-0.0, True), (1e-45, True), (1e-6, True), (1.0, True), (3.4e38, True), (-1e-45, False), (-1.0, False),
+                       (float("inf"), False), (float("-inf"), False), (float("nan"), False)):
+        p = lf.lf_axes_shape(12, 128, 4680, 0, 0, (22, 21, 21), eps, 0, 1536, 128, 128 * 4680)
+        assert (lib.lf_qk_norm_rope_axes_bwd_workspace_bytes(C.byref(p)) > 0) == taken, eps
+        want = ALIGN if taken else SHAPE
+        assert lib.lf_qk_norm_rope_axes(FAKE, FAKE, FAKE, FAKE, C.byref(p), FAKE + 2, None) == want, eps
+        assert lib.lf_qk_norm_rope_axes_bwd(FAKE, FAKE, FAKE, FAKE, C.byref(p), FAKE, FAKE + 2, FAKE, FAKE, 1 << 30, None) == want, eps
