@@ -390,7 +390,7 @@ int lf_qk_norm_rope(const void* X, const float* g, const float* cos_table, const
  *   Y[h][l] = R(theta[l]) (X[l][h] * inv * g[h]),   inv = 1 / sqrt(mean(x^2) + eps).
  * lf_qk_norm_rope_axes_bwd computes, for an upstream gradient dY and with z = R(-theta) dY, n = x * inv, u = z * g:
  *   dg = sum over tokens of z * n,     dX = inv * (u - n * mean(u * n)),
- * the mean over the channels that the norm takes.  float32 throughout, dX rounded once to bfloat16; sums in a fixed order
+ * the mean over the channels that the norm takes.  eps may be 0 (a token whose channels are all 0 then gives NaN).  float32 throughout, dX rounded once to bfloat16; sums in a fixed order
  * (no atomics: results are reproducible).
  * Arguments
  *   X        device, bfloat16 [tokens][>= H*d], row stride x_stride_tok elements.
@@ -463,7 +463,8 @@ int lf_kvq_read(const void* cache, size_t cache_bytes, const lf_kvq_shape* cache
  * [kv_len - q_len, kv_len) are read from them in bfloat16 ([H][q_len][d] with the k_ and v_ strides of `shape`), as
  * long as the chunk is being denoised, and only the history from the cache; with K and V both NULL all kv_len tokens
  * lie in the cache (the k_ and v_ strides are not looked at).
- * bf16 MFMA products on the values that the cache stands for, float32 softmax and accumulation, bfloat16 output.
+ * bf16 MFMA products on the values that the cache stands for, float32 softmax and accumulation, bfloat16 output; probabilities are
+ * rounded to bfloat16 for their product with V, and the row's sum is taken of the rounded ones.
  * Arguments
  *   Q, O, shape, indices, list_len, softmax_scale   as lf_sparse_attn (order of a list is free, invalid ids are skipped,
  *              duplicates count twice, rows without a valid id are zeros).

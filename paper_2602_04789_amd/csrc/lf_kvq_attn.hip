@@ -3,7 +3,8 @@
 //   O_x = sum_y softmax_y(q_x . k_y scale) v_y,   y over the tokens of the listed blocks, or over all tokens
 //
 // Few query rows share the cache's bytes, so HBM bounds the call (one row over 131 076 tokens of 12 x 128: 41 us, 5.2 TB/s of codes and scales),
-// or the chain of a tile where many rows share them (64 rows of 40 x 64 over 32 824 tokens: 43 us, 0.5 PFLOP/s).  A wavefront has up
+// or the work on a tile where many rows share them (64 rows of 40 x 64 over 32 824 tokens: 43 us, 0.5 PFLOP/s, 2.3 times what the bytes take): two
+// wavefronts that share the rows each convert and stage all of it.  A wavefront has up
 // to 32 rows of the block (33 to 64 rows: two wavefronts share them; all in one, with tiles half as long, took 55 us there) and tiles of 64 tokens of
 // its own: the tiles of a list are dealt out over the four wavefronts of `parts` workgroups, with an online softmax each and nothing shared until
 // the end, so no barrier stands in the loop.
@@ -180,9 +181,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void lf_kvq_attn_kernel(KvqAttnArgs
   bf16x8 ones;
 #pragma unroll
   for (int i = 0; i < 8; ++i) ones[i] = (__bf16)1.0f;
-  // Rows of V in LDS, 16-byte chunks swizzled so that neither side meets a bank twice: 16 lanes write one chunk (u) of every group of four rows
-  // (d = 64: eight), 32 lanes of the transposing read take 32 bytes (two chunks) of each of eight rows.  Pairs of chunks go by the row, the place
-  // in a pair by the group; 16 rows on it is the same.
+  // Rows of V in LDS, 16-byte chunks swizzled for 16 neighbouring lanes that write one chunk (u) of every group of four rows (d = 64:
+  // eight), and for 32 lanes of the transposing read that take 32 bytes (two chunks) of each of eight rows.  Pairs of chunks go by the row, the
+  // place in a pair by the group; 16 rows on it is the same.  52 -> 49 us on 64 rows x 40 x 64 over 32 824 tokens.  Not free of conflicts:
+  // 64 cycles of them a wavefront's tile at d = 64, 128 at d = 128, 39 % of the LDS cycles, as many as one of the two sides takes without any.
   auto swz = [](int row, int ch) __attribute__((always_inline)) {
     return ch ^ (CH == 16 ? (row & 7) << 1 : (row >> 1 & 3) << 1) ^ (ch >> 2 & 1);
   };

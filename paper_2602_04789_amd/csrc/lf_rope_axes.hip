@@ -10,8 +10,8 @@
 // A thread owns the 16-byte chunk `cih` (8 channels) of up to NI heads of one token, so it makes that chunk's angles once for
 // all of them.  The CH = d/8 chunks of a head are neighbouring lanes of one wavefront (64 is a multiple of CH): a head's
 // sums are taken across CH lanes, and the partner of a channel pair (i, i + d/2) is CH/2 lanes away.  Sums over all heads of a
-// token go through LDS.  All arithmetic is float32 but for the angles: they are products of float64, reduced to a
-// quarter turn there, so far positions keep their phase.
+// token go through LDS.  All arithmetic is float32 but for the angles: they are products of float64, reduced to
+// half a turn either way there, so far positions keep their phase.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
