@@ -489,7 +489,8 @@ int lf_sparse_attn_kvq(const void* Q, const void* cache, size_t cache_bytes, con
  * Attention of a few query rows (single tokens, or the query heads that share a cached head, as rows) over every token:
  *   O_x = sum_y softmax_y(q_x . k_y * softmax_scale) v_y,   y over the first cached_len tokens of the cache and the extra_len
  *   rows of K and V (bfloat16, [H][extra_len][d]; not looked at when extra_len = 0).  Every row sees every token.
- * The long axis is divided among workgroups and joined in a fixed order.  Without any token the rows are zeros.
+ * The long axis is divided among workgroups and joined in a fixed order.  Without any token the rows are zeros.  Arithmetic as
+ * lf_sparse_attn_kvq; up to 16 rows the probabilities keep 16 bits, so the rounding of O is what is left.
  * workspace and the rest as lf_sparse_attn_kvq.
  * Errors: LF_ERR_NULL; LF_ERR_SHAPE (q_len not in 1 .. 64, lengths negative or above 2^24, cached_len above the capacity, heads or head_dim
  *   unlike the cache's, heads of O that share an element); LF_ERR_ALIGN; LF_ERR_WORKSPACE; LF_ERR_HIP.

@@ -2,7 +2,7 @@
 //
 //   O_x = sum_y softmax_y(q_x . k_y scale) v_y,   y over the tokens of the listed blocks, or over all tokens
 //
-// Few query rows share the cache's bytes, so HBM bounds the call (one row over 131 076 tokens of 12 x 128: 41 us, 5.2 TB/s of codes and scales),
+// Few query rows share the cache's bytes, so HBM bounds the call (one row over 131 076 tokens of 12 x 128: 42 us, 5.1 TB/s of codes and scales),
 // or the work on a tile where many rows share them (64 rows of 40 x 64 over 32 824 tokens: 43 us, 0.5 PFLOP/s, 2.3 times what the bytes take): two
 // wavefronts that share the rows each convert and stage all of it.  A wavefront has up
 // to 32 rows of the block (33 to 64 rows: two wavefronts share them; all in one, with tiles half as long, took 55 us there) and tiles of 64 tokens of
@@ -18,7 +18,9 @@
 //
 // Softmax is float32 in the exp2 domain, P = exp2(s c - m), against a reference m per row that moves only when a tile's sum of P is large:
 // without that no lane asks another and no maximum of scores is taken.  P is rounded to bfloat16 for the product (as the output is); the
-// row's sum is the product of the same P with ones, in float32.
+// row's sum is the product of the same P with ones, in float32.  Up to 16 rows P goes into both products in two bfloat16 parts, 16 bits: bytes
+// bound these calls, so it costs little (one row over 131 076 tokens: 45.9 -> 46.9 us), and the output's 2-norm error falls from 2.6e-3 to the 1.7e-3
+// that its own rounding is.  With more rows, and in the bfloat16 kernels, one part is kept: the products and vector work are the bound there.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -84,6 +86,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void lf_kvq_attn_kernel(KvqAttnArgs
   constexpr int CH = D / 8;           // 16-byte chunks of a row in LDS
   constexpr int VI = D / 64;          // scaled groups of half a tile's V for a lane
   constexpr int SL = kWaves / RG;     // tiles at a time
+  constexpr bool TWO = NQ == 1;       // P in two bfloat16 parts: up to 16 rows
   __shared__ u32x4 stage[kWaves][32 * CH];
   __shared__ float2 ml[kWaves][16 * NQ];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -258,7 +261,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void lf_kvq_attn_kernel(KvqAttnArgs
 #pragma unroll
         for (int i = 0; i < 16; ++i) p[q][i] = __builtin_amdgcn_exp2f(fmaf(sacc[q][i >> 2][i & 3], a.c, -m_run[q]));
     };
-    bf16x8 pf[NQ][2];
+    bf16x8 pf[NQ][2], rest[2];
     f32x4 sum[NQ];
     auto sums = [&]() __attribute__((always_inline)) {
 #pragma unroll
@@ -300,19 +303,30 @@ __global__ __launch_bounds__(64 * kWaves, 2) void lf_kvq_attn_kernel(KvqAttnArgs
       sums();
       first = false;
     }
+    if constexpr (TWO) {      // what P's rounding left off (only now: before the reference has moved P may be infinite)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) rest[i >> 3][i & 7] = (__bf16)(p[0][i] - (float)pf[0][i >> 3][i & 7]);
+#pragma unroll
+      for (int half = 0; half < 2; ++half) sum[0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, rest[half], sum[0], 0, 0, 0);
+    }
 #pragma unroll
     for (int q = 0; q < NQ; ++q) l_run[q] += sum[q][0];
     auto product = [&](int half) __attribute__((always_inline)) {
       const uint16_t* v16 = reinterpret_cast<const uint16_t*>(vt);
+      bf16x8 vf[MB];
 #pragma unroll
       for (int mb = 0; mb < MB; ++mb) {
         const int vrow = 4 * kg + (col >> 2), vcol = 16 * mb + 4 * (col & 3);
         const int off = (vrow * CH + swz(vrow, vcol >> 3)) * 8 + (vcol & 7);      // (16 rows on the swizzle is the same)
         const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(LDS_PTR(bf16x4, v16 + off));
         const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(LDS_PTR(bf16x4, v16 + off + 16 * CH * 8));
-        const bf16x8 vf = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        vf[mb] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
 #pragma unroll
-        for (int q = 0; q < NQ; ++q) oacc[q][mb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[q][half], oacc[q][mb], 0, 0, 0);
+        for (int q = 0; q < NQ; ++q) oacc[q][mb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[mb], pf[q][half], oacc[q][mb], 0, 0, 0);
+      }
+      if constexpr (TWO) {      // (each sum's two products one behind the other: 48.1 us instead of 46.9)
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb) oacc[0][mb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[mb], rest[half], oacc[0][mb], 0, 0, 0);
       }
     };
     product(0);
