@@ -42,14 +42,14 @@ typedef enum {
   LF_ERR_NULL = -1,      /* a required pointer is NULL */
   LF_ERR_SHAPE = -2,     /* sizes inconsistent or unsupported (see lf_shape) */
   LF_ERR_BUDGET = -3,    /* budget inconsistent with the shape */
-  LF_ERR_DTYPE = -4,     /* dtype other than LF_BF16 */
+  LF_ERR_DTYPE = -4,     /* a dtype that the call does not take */
   LF_ERR_ALIGN = -5,     /* pointer or stride breaks the 16-byte row alignment */
   LF_ERR_WORKSPACE = -6, /* workspace NULL or smaller than lf_workspace_bytes() */
   LF_ERR_HIP = -7,       /* a kernel launch of this call failed */
   LF_ERR_SCHEDULE = -8   /* schedule fields out of range */
 } lf_status;
 
-typedef enum { LF_BF16 = 0 } lf_dtype;
+typedef enum { LF_BF16 = 0, LF_F32 = 1 /* only where a call says so */ } lf_dtype;
 
 /* How the per-chunk keep ratio is chosen. */
 typedef enum {
@@ -511,6 +511,138 @@ size_t lf_token_attn_kvq_workspace_bytes(const lf_token_shape* shape);
 int lf_token_attn_kvq(const void* Q, const void* cache, size_t cache_bytes, const lf_kvq_shape* cache_shape,
                       const void* K, const void* V, const lf_token_shape* shape, float softmax_scale, void* O,
                       void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Between two blocks of the generator: the block's output is gated onto the residual stream, and the stream is normalised, scaled and shifted
+ * for the next block.  For every token l, with g its group (the tokens of a frame or of a sequence, which share a modulation):
+ *   p  = B                                        or, with post_weight,  B / sqrt(mean(B^2) + eps) * post_weight
+ *   Xout = X + residual_scale * gate[g] * p       rounded to the stream's type; without B the stream is X and is not written
+ *   n  = (Xout - mean(Xout)) / sqrt(var(Xout) + eps)   (LF_NORM_LAYER)   or   Xout / sqrt(mean(Xout^2) + eps)   (LF_NORM_RMS),
+ *        of the stream as it is written
+ *   Y  = n * weight * (1 + scale[g]) + shift[g]   bfloat16
+ * post_weight, gate, weight, scale and shift may be NULL: without a gate, a weight and a scale their factor is 1, without a shift it is 0.  (An affine norm
+ * is one with a single group, its bias the shift.)
+ *   lf_gate_norm_bwd   for upstream gradients dY of Y and dXout of Xout (either may be NULL: zeros): with f = weight (1 + scale[g]), u = dY f,
+ *                        v = (u - mean(u) - n mean(u n)) / sqrt(var + eps)      (RMS: without mean(u), the root of mean(Xout^2) + eps)
+ *                        dX = dXout + v           (of X and, through the stream, of what came before),
+ *                        dB = residual_scale gate[g] (dXout + v), through the norm with post_weight likewise,
+ *                        dshift[g] = sum dY,  dscale[g] = sum dY n weight,  dweight = sum dY n (1 + scale[g]),
+ *                        dgate[g] = sum residual_scale p (dXout + v),  dpost_weight = sum residual_scale gate[g] (B / rms) (dXout + v)
+ *                      summed over the tokens of the group (of all groups).  Xout is what the forward call wrote (X where it had no B).
+ *                      What is NULL among dgate, dpost_weight, dweight, dscale and dshift is not computed; a group without tokens gets zeros.
+ * float32 arithmetic, sums in a fixed order (no atomics: results are reproducible), each output rounded once.
+ * Groups: group_len > 0: token l belongs to group l / group_len, and `starts` is not looked at.  group_len = 0: group g has the tokens
+ *   [starts[g], starts[g + 1]), starts int32 [groups + 1] in device memory, ascending, 0 .. tokens; tokens before the first and behind
+ *   the last group are neither read nor written.  starts is not checked: nothing outside the tensors is touched for any values, but
+ *   results are right for ascending ones only.
+ * Arguments
+ *   X, Xout, dXout, dX   device, stream_dtype (LF_BF16 or LF_F32), [tokens][channels] with the row strides x_stride (X) and xo_stride.  Xout
+ *              may be X, and dX may be dXout.
+ *   B, dB      device, bfloat16, row stride b_stride.       Y, dY   device, bfloat16, row stride y_stride.
+ *   gate, scale, shift    device, float32 [groups][channels] with their row strides.   dgate, dscale, dshift   float32 [groups][channels], contiguous.
+ *   post_weight, weight, dpost_weight, dweight   device, float32 [channels].
+ *   workspace  device scratch of >= lf_gate_norm_bwd_workspace_bytes(), 256-byte aligned.
+ *   All pointers 16-byte aligned (starts: 4), row strides at least channels and multiples of 8 (tables: of 4; with one group any).  Outputs overlap nothing else.
+ *   eps may be 0 (a token whose channels are all alike then gives NaN).
+ * Errors: LF_ERR_NULL (also gate, post_weight or dB without B, B without Xout; a gradient of what the call does not have); LF_ERR_SHAPE (tokens not in 1 .. 2^30,
+ *   channels not a multiple of 8 in 8 .. 16 384, groups not in 1 .. 2^24 or not enough for group_len, kind, eps or residual_scale not finite,
+ *   strides below channels or above 2^40, a backward call of more than 2^32 threads or 2^40 bytes of workspace); LF_ERR_DTYPE; LF_ERR_ALIGN; LF_ERR_WORKSPACE; LF_ERR_HIP.
+ */
+typedef enum { LF_NORM_LAYER = 0, LF_NORM_RMS = 1 } lf_norm_kind;
+typedef struct {
+  int32_t tokens, channels;
+  int32_t groups, group_len;
+  int32_t stream_dtype;     /* lf_dtype of X, Xout, dXout, dX */
+  int32_t kind;             /* lf_norm_kind */
+  float eps, residual_scale;
+  int64_t x_stride, xo_stride, b_stride, y_stride;      /* elements */
+  int64_t gate_stride, scale_stride, shift_stride;
+} lf_norm_shape;
+
+int lf_gate_norm(const void* X, const void* B, const float* gate, const float* post_weight, const float* weight,
+                 const float* scale, const float* shift, const int32_t* starts, const lf_norm_shape* shape, void* Xout,
+                 void* Y, void* hip_stream);
+size_t lf_gate_norm_bwd_workspace_bytes(const lf_norm_shape* shape);
+int lf_gate_norm_bwd(const void* Xout, const void* B, const float* gate, const float* post_weight, const float* weight,
+                     const float* scale, const int32_t* starts, const lf_norm_shape* shape, const void* dY, const void* dXout,
+                     void* dX, void* dB, float* dgate, float* dpost_weight, float* dweight, float* dscale, float* dshift,
+                     void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Attention over packed sequences of different lengths, heads of Q sharing heads of K and V, and its gradients.
+ * Sequence b has the rows [q_start[b], q_start[b + 1]) of Q and the tokens [kv_start[b], kv_start[b + 1]) of K and V; head h reads head
+ * h / (heads / kv_heads) of them.  With nq rows and nk tokens, row i of a sequence sees its first
+ *   causal = 0: nk tokens (a text; a prompt's image),
+ *   causal = 1: nk - nq + i + 1 tokens: the last row sees all, each row before it one less,
+ *   causal = u: the tokens up to the end of the chunk of u tokens that holds token nk - nq + i  (frames or chunks that see
+ *               themselves and those before them)
+ * and at most nk, at least none: with nq > nk the first rows see nothing.  Rows that see nothing are zeros and add nothing to the gradients.
+ *   O_x = sum_y softmax_y(q_x . k_y * softmax_scale) v_y        and with it, where lse2 is not NULL,
+ *   lse2_x = log2 sum_y exp2(q_x . k_y * softmax_scale * log2 e)   (+inf for a row that sees nothing).
+ * lf_packed_attn_bwd computes dQ, dK and dV as lf_sparse_attn_bwd does, the sums running over what the rows see and, for dK and dV, over the heads
+ * that share the head.  bf16 MFMA products with float32 accumulation, float32 online softmax; P and P (dP - delta) are rounded to bfloat16 before the
+ * accumulating products (calls of few rows keep 16 bits of P); sums in a fixed order (no atomics: results are reproducible); bfloat16 outputs.  A long axis
+ * is divided among workgroups where there are few rows and joined in a fixed order, so a row may differ between calls of other sizes by the order of sums.
+ * Rows and tokens before the first and behind the last sequence are not looked at, and what is written leaves them as they were.
+ * Arguments
+ *   Q, O, dO, dQ   device, bfloat16 [heads][q_len][head_dim], O and dO with the o_ strides, dQ with the q_ strides.
+ *   K, V, dK, dV   device, bfloat16 [kv_heads][kv_len][head_dim], dK and dV with the k_ and v_ strides.
+ *   q_start, kv_start   device, int32 [seqs + 1], ascending, 0 .. q_len and 0 .. kv_len.  Not checked: nothing outside the tensors is touched
+ *              for any values, but results are right for ascending ones only.
+ *   lse2       device, float32 [heads][q_len], contiguous; the forward call may be given NULL.
+ *   softmax_scale  0 selects 1 / sqrt(head_dim).
+ *   workspace  device scratch of >= lf_packed_attn_workspace_bytes() (lf_packed_attn_bwd_workspace_bytes()), 256-byte aligned, may be NULL where that is 0.
+ *              Calls that may overlap must not share it.
+ * Inputs must be finite.  Outputs overlap nothing else.
+ * Errors: LF_ERR_NULL; LF_ERR_SHAPE (head_dim not 64 or 128; kv_heads not in 1 .. 4 096 or heads no multiple of it in 1 .. 256 times it; seqs not in
+ *   1 .. 2^20; q_len and kv_len not in 0 .. 2^30; causal not in 0 .. 2^30; a token stride not in head_dim .. 2^20, a head stride not in 0 .. 2^44; heads of an
+ *   output that share an element; a call, forward or backward, of 2^24 workgroups or more; softmax_scale negative or not finite); LF_ERR_DTYPE; LF_ERR_ALIGN; LF_ERR_WORKSPACE; LF_ERR_HIP.
+ * q_len = 0 or kv_len = 0: rows are zeros, gradients of tokens are zeros.
+ */
+typedef struct {
+  int32_t heads, kv_heads, head_dim;
+  int32_t seqs;
+  int32_t q_len, kv_len;    /* rows of Q, tokens of K and V, of all sequences */
+  int32_t causal;
+  int32_t dtype;            /* LF_BF16 */
+  int64_t q_stride_tok, q_stride_head; /* elements; multiples of 8 */
+  int64_t k_stride_tok, k_stride_head;
+  int64_t v_stride_tok, v_stride_head;
+  int64_t o_stride_tok, o_stride_head;
+} lf_packed_shape;
+
+size_t lf_packed_attn_workspace_bytes(const lf_packed_shape* shape);
+int lf_packed_attn(const void* Q, const void* K, const void* V, const lf_packed_shape* shape, const int32_t* q_start,
+                   const int32_t* kv_start, float softmax_scale, void* O, float* lse2, void* workspace,
+                   size_t workspace_bytes, void* hip_stream);
+size_t lf_packed_attn_bwd_workspace_bytes(const lf_packed_shape* shape);
+int lf_packed_attn_bwd(const void* Q, const void* K, const void* V, const void* O, const void* dO, const float* lse2,
+                       const lf_packed_shape* shape, const int32_t* q_start, const int32_t* kv_start, float softmax_scale,
+                       void* dQ, void* dK, void* dV, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * The norm over the gradients of all parameters, and their scaling to a largest norm:
+ *   norm = sqrt(sum of the squares of all elements of all tensors),    out = x * min(1, max_norm / (norm + eps))
+ * Squares and their sum are taken in binary64, in a fixed order (reproducible); the factor is rounded to float32, each output once.  Where the norm is not finite the
+ * factor is 1: gradients in place stay as they were, and the caller sees it in `norm`.  max_norm = infinity takes the norm alone; in place nothing
+ * is written where the factor is 1.
+ *   tensors    host array of `count` tensors (read during the call): data and out are device memory of numel contiguous elements, LF_BF16 or LF_F32 each,
+ *              aligned to their element.  out = NULL: in place, and out_dtype is not looked at.  A tensor's out overlaps no other tensor.  numel may be 0.
+ *   norm       device, float32, one element, written (infinity above 3.4e38).
+ *   workspace  device scratch of >= lf_grad_workspace_bytes(count, sum of all numel), 256-byte aligned.
+ * Errors: LF_ERR_NULL; LF_ERR_SHAPE (count not in 0 .. 2^20, numel negative, more than 2^40 elements in all, max_norm or eps negative or NaN, eps infinite); LF_ERR_DTYPE;
+ *   LF_ERR_ALIGN; LF_ERR_WORKSPACE; LF_ERR_HIP.
+ */
+typedef struct {
+  const void* data;
+  void* out;
+  int64_t numel;
+  int32_t dtype, out_dtype;
+} lf_grad_tensor;
+
+size_t lf_grad_workspace_bytes(int32_t count, int64_t numel);
+int lf_grad_clip(const lf_grad_tensor* tensors, int32_t count, float max_norm, float eps, float* norm, void* workspace,
+                 size_t workspace_bytes, void* hip_stream);
 
 /* Static, NUL-terminated description of an lf_status value. */
 const char* lf_strerror(int status);

@@ -445,7 +445,7 @@ extern "C" const char* lf_strerror(int status) {
     case LF_ERR_NULL: return "a required pointer is NULL";
     case LF_ERR_SHAPE: return "shape inconsistent or unsupported";
     case LF_ERR_BUDGET: return "budget inconsistent with the shape or beyond kernel limits";
-    case LF_ERR_DTYPE: return "unsupported dtype (bfloat16 only)";
+    case LF_ERR_DTYPE: return "unsupported dtype";
     case LF_ERR_ALIGN: return "pointer or stride not 16-byte aligned";
     case LF_ERR_WORKSPACE: return "workspace missing or too small";
     case LF_ERR_HIP: return "HIP kernel launch failed";

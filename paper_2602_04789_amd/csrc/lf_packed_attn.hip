@@ -1,0 +1,301 @@
+// Attention over packed sequences, and the joining of divided rows.
+//
+//   O_x = sum_y softmax_y(q_x . k_y scale) v_y,   y over the first tokens of x's sequence: all of them, or those up to its own or its chunk's end
+//
+// A workgroup of four wavefronts has 128 rows of one head, 32 of a wavefront, and walks the tokens that its last row sees in tiles of 64 that the
+// wavefronts share through LDS (two stages; the next tile is on its way while one is worked on).  The products are computed transposed,
+// S^T = K Q^T and O^T = V^T P^T with v_mfma_f32_32x32x16_bf16: a lane holds one row's scores of half the tokens, P stays in its registers as
+// the second product's operand, and V is read through the transposing LDS read.  The online softmax has a reference that moves only when a row's sum
+// is about to leave the range (see lf_attn.hip), so no maximum is taken on the way.  Only tiles that a wavefront's first row does not see whole are masked, and
+// those that its last row does not see are left out.
+//
+// Heads of the last rows, which see most, go first; neighbouring workgroups take heads in turn, so that those that share a head of K and V run at
+// one time on the XCDs that have it.
+#include "lf_packed.h"
+
+namespace {
+
+constexpr int kRows = 128;        // of a workgroup
+constexpr int kTok = 64;          // tokens of a tile
+
+template <int CH> __device__ __forceinline__ int v_swz(int row, int ch) {
+  return CH == 16 ? ch ^ ((row & 3) << 2) : ch ^ (((row >> 1) & 1) << 2);
+}
+
+template <int D>
+__global__ __launch_bounds__(256, 2) void lf_packed_attn_kernel(PackedArgs a) {
+  constexpr int CH = D / 8, KS = D / 16, MB = D / 32;
+  constexpr int TILE = kTok * CH;           // 16-byte chunks of K or V of a tile
+  constexpr int LPW = TILE / 64 / 4;        // load instructions of a wavefront for K or V of a tile
+  constexpr int RPI = 64 / CH;              // rows of a load instruction
+  __shared__ u32x4 stage[2][2 * TILE];      // K | V
+
+  int x = blockIdx.x;
+  const int hk = x % a.Hk;
+  x /= a.Hk;
+  const int h = hk * a.G + x % a.G;
+  x /= a.G;
+  const int part = x % a.parts, place = a.slots - 1 - x / a.parts;
+  int tile;
+  const int b = find_tile(a.q_start, a.seqs, a.q_len, 1, kRows, place, tile);
+  const Span s = span_of(a, b);
+  const int i0 = tile * kRows;
+  if (tile < 0 || i0 >= s.nq) return;
+  const int rows = min(kRows, s.nq - i0);
+
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int ln = lane & 31, kg = lane >> 5;
+  const int row = 32 * wave + ln;
+  // tokens that this lane's row, the wavefront's first and last and the workgroup's last row see
+  const int lim = row_limit(s, a.unit, min(i0 + row, s.nq - 1));
+  const bool active = 32 * wave < rows;
+  const int lim_first = row_limit(s, a.unit, i0 + 32 * wave);
+  const int lim_last = active ? row_limit(s, a.unit, i0 + min(32 * wave + 31, rows - 1)) : 0;
+  const int seen = row_limit(s, a.unit, i0 + rows - 1);
+  int t0 = 0, t1 = seen;
+  if (a.parts > 1) {
+    const int len = part_len(a, seen);
+    t0 = (int)min((int64_t)part * len, (int64_t)seen);
+    t1 = (int)min((int64_t)t0 + len, (int64_t)seen);
+    if (t0 >= t1) return;                 // the joining launch leaves it out too
+  }
+
+  Frag qf[KS];
+  {
+    const uint16_t* qp = a.Q + (int64_t)h * a.q_head + (int64_t)(s.q0 + i0 + row) * a.q_tok;
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+      qf[k].u = u32x4{0, 0, 0, 0};
+      if (row < rows) qf[k].u = *reinterpret_cast<const u32x4*>(qp + 16 * k + 8 * kg);
+    }
+  }
+  const uint16_t* Kh = a.K + (int64_t)hk * a.k_head;
+  const uint16_t* Vh = a.V + (int64_t)hk * a.v_head;
+  const uint32_t k_row = (uint32_t)(a.k_tok * 2), v_row = (uint32_t)(a.v_tok * 2);
+  uint32_t koff[LPW], voff[LPW];
+#pragma unroll
+  for (int i = 0; i < LPW; ++i) {
+    const int r = RPI * (LPW * wave + i) + lane / CH, p = lane % CH;
+    koff[i] = (uint32_t)r * k_row + (uint32_t)row_swz<CH>(r, p) * 16u - 1024u * (i & 3);
+    voff[i] = (uint32_t)r * v_row + (uint32_t)v_swz<CH>(r, p) * 16u - 1024u * (i & 3);
+  }
+  auto request = [&](int t, u32x4* to) __attribute__((always_inline)) {
+    const int n = min(kTok, t1 - t);
+    fetch<LPW>(rows_rsrc(Kh, (int64_t)s.k0 + t, n, k_row), lds_addr(to + LPW * 64 * wave), koff);
+    fetch<LPW>(rows_rsrc(Vh, (int64_t)s.k0 + t, n, v_row), lds_addr(to + TILE + LPW * 64 * wave), voff);
+  };
+  int kaddr[KS], vbase[MB];
+#pragma unroll
+  for (int k = 0; k < KS; ++k) kaddr[k] = ln * CH + row_swz<CH>(ln, 2 * k + kg);
+  {
+    const int i16 = lane & 15, tr_row = 4 * kg + (i16 >> 2), tr_col = 16 * ((lane >> 4) & 1) + 4 * (i16 & 3);
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb) {
+      const int col = 32 * mb + tr_col;
+      vbase[mb] = (tr_row * CH + v_swz<CH>(tr_row, col >> 3)) * 8 + (col & 7);
+    }
+  }
+
+  f32x16 oacc[MB];
+#pragma unroll
+  for (int mb = 0; mb < MB; ++mb) oacc[mb] = zero16();
+  constexpr float kSumMax = 1.0e30f;
+  float m_run = -1.0e30f, l_run = 0.0f;
+  auto row_max = [](const f32x16& x) __attribute__((always_inline)) {
+    float m = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
+#pragma unroll
+    for (int i = 4; i < 16; i += 2) m = fmaxf(m, fmaxf(x[i], x[i + 1]));
+    return m;
+  };
+  const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
+
+  // One tile of tokens [t, t + 64) of the sequence.
+  auto work = [&](int t, const u32x4* at) __attribute__((always_inline)) {
+    f32x16 sc[2];
+#pragma unroll
+    for (int hf = 0; hf < 2; ++hf) {
+      Frag kf[KS];
+#pragma unroll
+      for (int k = 0; k < KS; ++k) kf[k].u = at[kaddr[k] + 32 * hf * CH];
+      sc[hf] = zero16();
+#pragma unroll
+      for (int k = 0; k < KS; ++k) sc[hf] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[k].v, qf[k].v, sc[hf], 0, 0, 0);
+    }
+    if (t + kTok > lim_first) {      // accumulator i: token 8 (i / 4) + 4 kg + i mod 4 of the half tile
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (t + 32 * hf + 8 * (i >> 2) + 4 * kg + (i & 3) >= lim) sc[hf][i] = -INFINITY;
+    }
+    bf16x8 pf[4];
+    float l_new;
+    auto softmax = [&](float l0) __attribute__((always_inline)) {
+      l_new = l0;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) pf[u][e] = (__bf16)__builtin_amdgcn_exp2f(fmaf(sc[u >> 1][8 * (u & 1) + e], a.c, -m_run));
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) {
+          const bf16x2 pr = {pf[u][e], pf[u][e + 1]};
+          l_new = __builtin_amdgcn_fdot2_f32_bf16(pr, ones, l_new, false);
+        }
+      }
+    };
+    softmax(l_run);
+    if (__ballot(l_new > kSumMax) != 0ull) {
+      float top = fmaxf(row_max(sc[0]), row_max(sc[1]));
+      const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+      top = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * a.c;
+      const float m_new = fmaxf(m_run, top), alpha = __builtin_amdgcn_exp2f(m_run - m_new);
+      m_run = m_new;
+#pragma unroll
+      for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) oacc[mb][i] *= alpha;
+      softmax(l_run * alpha);
+    }
+    l_run = l_new;
+    const uint16_t* v16 = reinterpret_cast<const uint16_t*>(at + TILE);
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+#pragma unroll
+      for (int mb = 0; mb < MB; ++mb) {
+        const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(LDS_PTR(bf16x4, v16 + vbase[mb] + 16 * u * CH * 8));
+        const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(LDS_PTR(bf16x4, v16 + vbase[mb] + (16 * u + 8) * CH * 8));
+        oacc[mb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7), pf[u], oacc[mb], 0, 0, 0);
+      }
+  };
+  if (t0 < t1) request(t0, stage[0]);
+  int cur = 0;
+  for (int t = t0; t < t1; t += kTok, cur ^= 1) {
+    __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));     // this wavefront's share of the tile
+    lds_barrier();                                // everyone's, and nobody reads the other stage any more
+    if (t + kTok < t1) request(t + kTok, stage[cur ^ 1]);
+    if (t < lim_last) work(t, stage[cur]);
+  }
+
+  const float l = l_run + __shfl_xor(l_run, 32);
+  if (row >= rows) return;
+  if (a.parts > 1) {
+    const int64_t at = (((int64_t)place * a.H + h) * a.parts + part) * kRows + row;
+    if (kg == 0) a.state_ml[at] = make_float2(m_run, l);
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        f32x4 o;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = oacc[mb][4 * g + e];
+        *reinterpret_cast<f32x4*>(a.state_o + at * D + 32 * mb + 8 * g + 4 * kg) = o;
+      }
+    return;
+  }
+  const int64_t token = (int64_t)s.q0 + i0 + row;
+  const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+  if (a.lse2 && kg == 0) a.lse2[(int64_t)h * a.q_len + token] = l > 0.0f ? m_run + __builtin_log2f(l) : INFINITY;
+  uint16_t* op = a.O + (int64_t)h * a.o_head + token * a.o_tok;
+#pragma unroll
+  for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      bf16x4 o4;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o4[e] = (__bf16)(oacc[mb][4 * g + e] * inv);
+      *reinterpret_cast<bf16x4*>(op + 32 * mb + 8 * g + 4 * kg) = o4;
+    }
+}
+
+// Joins the parts of a row: a wavefront each, lane p holding part p's weight.  FEW: the row is a row and head of a tile of the few-row kernel.
+template <int D>
+__global__ __launch_bounds__(256) void lf_packed_join_kernel(PackedArgs a, int tile_rows, int few) {
+  constexpr int W = D / 64;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int groups = tile_rows / 4;           // workgroups of a tile: four rows each
+  const int64_t x = blockIdx.x;
+  const int r = 4 * (int)(x % groups) + wave, heads = few ? a.Hk : a.H;
+  const int64_t t = x / groups;
+  const int hh = (int)(t % heads), place = (int)(t / heads), mul = few ? a.G : 1;
+  int tile;
+  const int b = find_tile(a.q_start, a.seqs, a.q_len, mul, tile_rows, place, tile);
+  const Span s = span_of(a, b);
+  const int64_t i0 = (int64_t)tile * tile_rows, all = (int64_t)s.nq * mul;
+  if (tile < 0 || i0 + r >= all) return;
+  const int i = (int)((i0 + r) / mul), h = few ? hh * a.G + (int)((i0 + r) % mul) : hh;
+  const int seen = row_limit(s, a.unit, (int)((min(i0 + tile_rows, all) - 1) / mul));
+  const int len = part_len(a, seen), parts = (seen + len - 1) / len;
+  const int64_t first = t * a.parts * tile_rows + r;
+  float2 ml = make_float2(-INFINITY, 0.0f);
+  if (lane < parts) ml = a.state_ml[first + (int64_t)lane * tile_rows];
+  float M = ml.x;
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) M = fmaxf(M, __shfl_xor(M, off));
+  const float w = ml.y > 0.0f ? __builtin_amdgcn_exp2f(ml.x - M) : 0.0f;
+  float L = w * ml.y;
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) L += __shfl_xor(L, off);
+  float o[W];
+#pragma unroll
+  for (int e = 0; e < W; ++e) o[e] = 0.0f;
+  for (int p0 = 0; p0 < parts; p0 += 8) {
+    float v[8][W];
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+#pragma unroll
+      for (int e = 0; e < W; ++e) v[k][e] = p0 + k < parts ? a.state_o[(first + (int64_t)(p0 + k) * tile_rows) * D + W * lane + e] : 0.0f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const float wk = __shfl(w, p0 + k);
+#pragma unroll
+      for (int e = 0; e < W; ++e) o[e] = fmaf(wk, v[k][e], o[e]);
+    }
+  }
+  const float inv = L > 0.0f ? 1.0f / L : 0.0f;
+  const int64_t token = (int64_t)s.q0 + i;
+  if (a.lse2 && lane == 0) a.lse2[(int64_t)h * a.q_len + token] = L > 0.0f ? M + __builtin_log2f(L) : INFINITY;
+  __bf16* to = reinterpret_cast<__bf16*>(a.O + (int64_t)h * a.o_head + token * a.o_tok) + W * lane;
+#pragma unroll
+  for (int e = 0; e < W; ++e) to[e] = (__bf16)(o[e] * inv);
+}
+
+}  // namespace
+
+PackedArgs lf_packed_args(const lf_packed_call* c) {
+  const lf_packed_shape* s = c->s;
+  PackedArgs a = {};
+  a.Q = (const uint16_t*)c->Q; a.K = (const uint16_t*)c->K; a.V = (const uint16_t*)c->V; a.dO = (const uint16_t*)c->dO;
+  a.O = (uint16_t*)c->O; a.dQ = (uint16_t*)c->dQ; a.dK = (uint16_t*)c->dK; a.dV = (uint16_t*)c->dV;
+  a.lse2 = c->lse2;
+  a.q_start = c->q_start; a.kv_start = c->kv_start;
+  a.q_tok = s->q_stride_tok; a.q_head = s->q_stride_head; a.k_tok = s->k_stride_tok; a.k_head = s->k_stride_head;
+  a.v_tok = s->v_stride_tok; a.v_head = s->v_stride_head; a.o_tok = s->o_stride_tok; a.o_head = s->o_stride_head;
+  a.H = s->heads; a.Hk = s->kv_heads; a.G = s->heads / s->kv_heads;
+  a.seqs = s->seqs; a.q_len = s->q_len; a.kv_len = s->kv_len; a.unit = s->causal;
+  a.slots = (int)c->plan.slots; a.parts = c->plan.parts; a.part_tokens = c->plan.part_tokens;
+  a.scale = c->scale;
+  a.c = c->scale * 1.44269504088896340736f;
+  const int64_t states = c->plan.slots * (c->plan.few ? a.Hk : a.H) * c->plan.parts * c->plan.tile;
+  a.state_o = (float*)c->workspace;
+  a.state_ml = (float2*)((float*)c->workspace + states * s->head_dim);
+  return a;
+}
+
+int lf_launch_packed_join(const PackedArgs& a, int d, int tile_rows, bool few, hipStream_t st) {
+  const dim3 grid((unsigned)((int64_t)a.slots * (few ? a.Hk : a.H) * (tile_rows / 4)));
+  const hipError_t rc = d == 128 ? lf_launch(lf_packed_join_kernel<128>, grid, dim3(256), 0, st, a, tile_rows, (int)few)
+                                 : lf_launch(lf_packed_join_kernel<64>, grid, dim3(256), 0, st, a, tile_rows, (int)few);
+  return rc == hipSuccess ? LF_OK : LF_ERR_HIP;
+}
+
+int lf_launch_packed_attn(const lf_packed_call* c, void* stream) {
+  if (c->plan.few) return lf_launch_packed_rows(c, stream);
+  const PackedArgs a = lf_packed_args(c);
+  const int d = c->s->head_dim;
+  hipStream_t st = (hipStream_t)stream;
+  const dim3 grid((unsigned)((int64_t)a.slots * a.H * a.parts));
+  const hipError_t rc = d == 128 ? lf_launch(lf_packed_attn_kernel<128>, grid, dim3(256), 0, st, a)
+                                 : lf_launch(lf_packed_attn_kernel<64>, grid, dim3(256), 0, st, a);
+  if (rc != hipSuccess) return LF_ERR_HIP;
+  return a.parts > 1 ? lf_launch_packed_join(a, d, kRows, false, st) : LF_OK;
+}

@@ -1,0 +1,420 @@
+// Backward pass of the packed attention.  With P = exp2(s c - lse2), delta_x = dO_x . O_x, dP = dO V^T, dS = P (dP - delta):
+//   dV_y = sum_x P dO_x      dQ_x = scale sum_y dS k_y      dK_y = scale sum_x dS q_x     (dK and dV over the heads that share the head, too)
+//
+// No atomics, every launch owns its outputs: one leaves -delta, one owns rows and walks the tokens they see (dQ), one owns tokens and walks the
+// rows that see them, head by head (dK, dV).  Both recompute the scores.  As in the forward kernel the score-like products take their A operand from tiles in
+// LDS and their B operand from the owner's rows in registers; P and dS are then the B operand of the accumulating products, whose A operand
+// is the same tile through the transposing read.  Matrix work bounds both: seven products for the five that the mathematics counts.
+#include "lf_packed.h"
+
+namespace {
+
+constexpr int kTile = 32;         // streamed rows of a step
+
+// One swizzle for tiles that are read both ways (rows, and transposed: half a wavefront takes four chunks of each of four rows); the transposing
+// read of rows 8 .. 15 of 16 sees chunk bit 1 flipped where a row is 256 bytes.
+template <int CH> __device__ __forceinline__ int both_swz(int row, int ch) {
+  return CH == 16 ? ch ^ (((row & 3) << 2) | ((row >> 2) & 3)) : ch ^ ((row & 1) << 2);
+}
+template <int CH> constexpr int kTrHiFlip = CH == 16 ? 16 : 0;
+
+// -delta of every row of every sequence: CH lanes a row.
+template <int D>
+__global__ __launch_bounds__(256) void lf_packed_delta_kernel(PackedArgs a) {
+  constexpr int CH = D / 8;
+  const int64_t x = (int64_t)blockIdx.x * (256 / CH) + threadIdx.x / CH;
+  if (x >= (int64_t)a.H * a.q_len) return;
+  const int h = (int)(x / a.q_len), ch = threadIdx.x % CH;
+  const int64_t i = x % a.q_len;
+  const int64_t at = (int64_t)h * a.o_head + i * a.o_tok + 8 * ch;
+  const u32x4 o = *reinterpret_cast<const u32x4*>(a.O + at), g = *reinterpret_cast<const u32x4*>(a.dO + at);
+  float v = 0.0f;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    v = fmaf(__uint_as_float(o[e] << 16), __uint_as_float(g[e] << 16), v);
+    v = fmaf(__uint_as_float(o[e] & 0xffff0000u), __uint_as_float(g[e] & 0xffff0000u), v);
+  }
+#pragma unroll
+  for (int off = 1; off < CH; off <<= 1) v += __shfl_xor(v, off);
+  if (ch == 0) a.ndelta[x] = -v;
+}
+
+// dQ: four wavefronts of 32 rows each share tiles of 32 tokens of K and V.
+template <int D>
+__global__ __launch_bounds__(256, 2) void lf_packed_dq_kernel(PackedArgs a) {
+  constexpr int kRows = 128;
+  constexpr int CH = D / 8, KS = D / 16, MB = D / 32;
+  constexpr int T32 = kTile * CH;
+  constexpr int LPW = T32 / 64 / 4;
+  constexpr int RPI = 64 / CH;
+  __shared__ u32x4 stage[2][2 * T32];      // K | V
+
+  int x = blockIdx.x;
+  const int hk = x % a.Hk;
+  x /= a.Hk;
+  const int h = hk * a.G + x % a.G, place = a.slots - 1 - x / a.G;
+  int tile;
+  const int b = find_tile(a.q_start, a.seqs, a.q_len, 1, kRows, place, tile);
+  const Span s = span_of(a, b);
+  const int i0 = tile * kRows;
+  if (tile < 0 || i0 >= s.nq) return;
+  const int rows = min(kRows, s.nq - i0);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int ln = lane & 31, kg = lane >> 5;
+  const int row = 32 * wave + ln;
+  const bool ok = row < rows;
+  const int64_t token = (int64_t)s.q0 + i0 + row;
+  const int lim = row_limit(s, a.unit, min(i0 + row, s.nq - 1));
+  const bool active = 32 * wave < rows;
+  const int lim_first = row_limit(s, a.unit, i0 + 32 * wave);
+  const int lim_last = active ? row_limit(s, a.unit, i0 + min(32 * wave + 31, rows - 1)) : 0;
+  const int seen = row_limit(s, a.unit, i0 + rows - 1);
+
+  Frag qf[KS], gf[KS];
+#pragma unroll
+  for (int k = 0; k < KS; ++k) {
+    qf[k].u = gf[k].u = u32x4{0, 0, 0, 0};
+    if (ok) {
+      qf[k].u = *reinterpret_cast<const u32x4*>(a.Q + (int64_t)h * a.q_head + token * a.q_tok + 16 * k + 8 * kg);
+      gf[k].u = *reinterpret_cast<const u32x4*>(a.dO + (int64_t)h * a.o_head + token * a.o_tok + 16 * k + 8 * kg);
+    }
+  }
+  float lse = INFINITY, nd = 0.0f;
+  if (ok) {
+    lse = a.lse2[(int64_t)h * a.q_len + token];
+    nd = a.ndelta[(int64_t)h * a.q_len + token];
+  }
+  const uint16_t* Kh = a.K + (int64_t)hk * a.k_head;
+  const uint16_t* Vh = a.V + (int64_t)hk * a.v_head;
+  const uint32_t k_row = (uint32_t)(a.k_tok * 2), v_row = (uint32_t)(a.v_tok * 2);
+  uint32_t koff[LPW], voff[LPW];
+#pragma unroll
+  for (int i = 0; i < LPW; ++i) {
+    const int r = RPI * (LPW * wave + i) + lane / CH, p = lane % CH;
+    koff[i] = (uint32_t)r * k_row + (uint32_t)both_swz<CH>(r, p) * 16u - 1024u * (i & 3);
+    voff[i] = (uint32_t)r * v_row + (uint32_t)row_swz<CH>(r, p) * 16u - 1024u * (i & 3);
+  }
+  auto request = [&](int t, u32x4* to) __attribute__((always_inline)) {
+    const int n = min(kTile, seen - t);
+    fetch<LPW>(rows_rsrc(Kh, (int64_t)s.k0 + t, n, k_row), lds_addr(to + LPW * 64 * wave), koff);
+    fetch<LPW>(rows_rsrc(Vh, (int64_t)s.k0 + t, n, v_row), lds_addr(to + T32 + LPW * 64 * wave), voff);
+  };
+  int kaddr[KS], vaddr[KS], tbase[MB];
+#pragma unroll
+  for (int k = 0; k < KS; ++k) {
+    kaddr[k] = ln * CH + both_swz<CH>(ln, 2 * k + kg);
+    vaddr[k] = ln * CH + row_swz<CH>(ln, 2 * k + kg);
+  }
+  {
+    const int i16 = lane & 15, tr_row = 4 * kg + (i16 >> 2), tr_col = 16 * ((lane >> 4) & 1) + 4 * (i16 & 3);
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb) {
+      const int col = 32 * mb + tr_col;
+      tbase[mb] = (tr_row * CH + both_swz<CH>(tr_row, col >> 3)) * 8 + (col & 7);
+    }
+  }
+  f32x16 acc[MB], nd16;
+#pragma unroll
+  for (int mb = 0; mb < MB; ++mb) acc[mb] = zero16();
+#pragma unroll
+  for (int i = 0; i < 16; ++i) nd16[i] = nd;
+
+  auto work = [&](int t, const u32x4* at) __attribute__((always_inline)) {
+    Frag kf[KS], vf[KS];
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+      kf[k].u = at[kaddr[k]];
+      vf[k].u = at[T32 + vaddr[k]];
+    }
+    f32x16 sc = zero16(), dp = nd16;
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+      sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[k].v, qf[k].v, sc, 0, 0, 0);
+      dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[k].v, gf[k].v, dp, 0, 0, 0);
+    }
+    if (t + kTile > lim_first) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (t + 8 * (i >> 2) + 4 * kg + (i & 3) >= lim) sc[i] = -INFINITY;
+    }
+    bf16x8 ds[2];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) ds[i >> 3][i & 7] = (__bf16)(__builtin_amdgcn_exp2f(fmaf(sc[i], a.c, -lse)) * dp[i]);
+    const uint16_t* k16 = reinterpret_cast<const uint16_t*>(at);
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int mb = 0; mb < MB; ++mb) {
+        const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(LDS_PTR(bf16x4, k16 + tbase[mb] + 16 * u * CH * 8));
+        const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(LDS_PTR(bf16x4, k16 + (tbase[mb] ^ kTrHiFlip<CH>) + (16 * u + 8) * CH * 8));
+        acc[mb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7), ds[u], acc[mb], 0, 0, 0);
+      }
+  };
+  if (seen > 0) request(0, stage[0]);
+  int cur = 0;
+  for (int t = 0; t < seen; t += kTile, cur ^= 1) {
+    __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+    lds_barrier();
+    if (t + kTile < seen) request(t + kTile, stage[cur ^ 1]);
+    if (t < lim_last) work(t, stage[cur]);
+  }
+  if (!ok) return;
+  uint16_t* op = a.dQ + (int64_t)h * a.q_head + token * a.q_tok;
+#pragma unroll
+  for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      bf16x4 o4;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o4[e] = (__bf16)(acc[mb][4 * g + e] * a.scale);
+      *reinterpret_cast<bf16x4*>(op + 32 * mb + 8 * g + 4 * kg) = o4;
+    }
+}
+
+// dK and dV of 64 tokens: wavefront (rh, role) has 32 of them.  Role 0 computes S = Q K^T, P and dV^T += dO^T P, role 1 dP = dO V^T, dS and
+// dK^T += Q^T dS a step later, with the P that its partner has left in LDS; so a tile of rows lives for two steps (three stages), and one barrier a step
+// is enough.
+template <int D>
+__global__ __launch_bounds__(256, 2) void lf_packed_dkv_kernel(PackedArgs a) {
+  constexpr int kTokens = 64;
+  constexpr int CH = D / 8, KS = D / 16, MB = D / 32;
+  constexpr int T32 = kTile * CH;
+  constexpr int LPW = T32 / 64 / 4;
+  constexpr int RPI = 64 / CH;
+  __shared__ u32x4 buf[3][2 * T32];          // [step mod 3][Q | dO]
+  __shared__ f32x4 st[3][4][16];             // lse2 (role 0) or -delta of the 32 rows, for each wavefront; the upper half takes what the other lanes load
+  __shared__ u32x4 ph[2][2][2][64];          // P: [step parity][rh][k-step][lane]
+
+  int x = blockIdx.x;
+  const int hk = x % a.Hk, place = x / a.Hk;
+  int tile;
+  const int b = find_tile(a.kv_start, a.seqs, a.kv_len, 1, kTokens, place, tile);
+  const Span s = span_of(a, b);
+  const int j0 = tile * kTokens;
+  if (tile < 0 || j0 >= s.nk) return;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int ln = lane & 31, kg = lane >> 5, rh = wave & 1;
+  const bool is_ds = wave >= 2;
+  const int j = j0 + 32 * rh + ln;
+  const bool ok = j < s.nk;
+  const int64_t token = (int64_t)s.k0 + j;
+  // the first rows that see this lane's token, the wavefront's last one and the workgroup's first one
+  const int from = first_row(s, a.unit, j), from_last = first_row(s, a.unit, min(j0 + 32 * rh + 31, s.nk - 1));
+  const int i_first = first_row(s, a.unit, j0) / kTile * kTile;
+  const int tiles = i_first < s.nq ? (s.nq - i_first + kTile - 1) / kTile : 0, steps_all = tiles;
+
+  Frag of[KS];
+  {
+    const uint16_t* p = is_ds ? a.V + (int64_t)hk * a.v_head + token * a.v_tok : a.K + (int64_t)hk * a.k_head + token * a.k_tok;
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+      of[k].u = u32x4{0, 0, 0, 0};
+      if (ok) of[k].u = *reinterpret_cast<const u32x4*>(p + 16 * k + 8 * kg);
+    }
+  }
+  const uint32_t q_row = (uint32_t)(a.q_tok * 2), o_row = (uint32_t)(a.o_tok * 2);
+  uint32_t qoff[LPW], ooff[LPW];
+#pragma unroll
+  for (int i = 0; i < LPW; ++i) {
+    const int r = RPI * (LPW * wave + i) + lane / CH, p = lane % CH;
+    qoff[i] = (uint32_t)r * q_row + (uint32_t)both_swz<CH>(r, p) * 16u - 1024u * (i & 3);
+    ooff[i] = (uint32_t)r * o_row + (uint32_t)both_swz<CH>(r, p) * 16u - 1024u * (i & 3);
+  }
+  const uint32_t st_off = (uint32_t)lane * 4u;
+  const float* stat = is_ds ? a.ndelta : a.lse2;
+  // where the next request goes: rows [ri, ri + 32) of the sequence, head rg of the group
+  int ri = i_first, rg = 0;
+  auto request = [&](int to) __attribute__((always_inline)) {
+    const int h = hk * a.G + rg, n = min(kTile, s.nq - ri);
+    const int64_t first = (int64_t)s.q0 + ri;
+    fetch<LPW>(rows_rsrc(a.Q + (int64_t)h * a.q_head, first, n, q_row), lds_addr(buf[to] + LPW * 64 * wave), qoff);
+    fetch<LPW>(rows_rsrc(a.dO + (int64_t)h * a.o_head, first, n, o_row), lds_addr(buf[to] + T32 + LPW * 64 * wave), ooff);
+    const int32x4 rs = aged(rows_rsrc(reinterpret_cast<const uint16_t*>(stat + (int64_t)h * a.q_len), first, n, 4u));
+    const uint32_t at = __builtin_amdgcn_readfirstlane(lds_addr(st[to][wave]));
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" :: "s"(at), "v"(st_off), "s"(rs) : "memory", "m0");
+    ri += kTile;
+    if (ri >= s.nq) {
+      ri = i_first;
+      ++rg;
+    }
+  };
+  int raddr[KS], tbase[MB];
+#pragma unroll
+  for (int k = 0; k < KS; ++k) raddr[k] = ln * CH + both_swz<CH>(ln, 2 * k + kg);
+  {
+    const int i16 = lane & 15, tr_row = 4 * kg + (i16 >> 2), tr_col = 16 * ((lane >> 4) & 1) + 4 * (i16 & 3);
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb) {
+      const int col = 32 * mb + tr_col;
+      tbase[mb] = (tr_row * CH + both_swz<CH>(tr_row, col >> 3)) * 8 + (col & 7);
+    }
+  }
+  f32x16 acc[MB];
+#pragma unroll
+  for (int mb = 0; mb < MB; ++mb) acc[mb] = zero16();
+
+  auto tfrag = [&](const u32x4* at, int u, int mb) __attribute__((always_inline)) {
+    const uint16_t* p = reinterpret_cast<const uint16_t*>(at);
+    const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(LDS_PTR(bf16x4, p + tbase[mb] + 16 * u * CH * 8));
+    const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(LDS_PTR(bf16x4, p + (tbase[mb] ^ kTrHiFlip<CH>) + (16 * u + 8) * CH * 8));
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  };
+  auto rows_of = [&](const u32x4* at, Frag (&f)[KS]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int k = 0; k < KS; ++k) f[k].u = at[raddr[k]];
+  };
+  auto product = [&](const Frag (&f)[KS], f32x16 c) __attribute__((always_inline)) {
+#pragma unroll
+    for (int k = 0; k < KS; ++k) c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[k].v, of[k].v, c, 0, 0, 0);
+    return c;
+  };
+  auto first_half = [&](const u32x4* at, bf16x8 (&tf)[MB]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb) tf[mb] = tfrag(at, 0, mb);
+  };
+  auto accumulate = [&](const u32x4* at, const bf16x8 (&tf)[MB], const bf16x8 (&y)[2]) __attribute__((always_inline)) {
+    bf16x8 t2[MB];
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb) t2[mb] = tfrag(at, 1, mb);
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb) acc[mb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tf[mb], y[0], acc[mb], 0, 0, 0);
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb) acc[mb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(t2[mb], y[1], acc[mb], 0, 0, 0);
+  };
+  auto stats16 = [&](int at) __attribute__((always_inline)) {
+    f32x16 v;
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const f32x4 y = st[at][wave][2 * g + kg];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[4 * g + e] = y[e];
+    }
+    return v;
+  };
+  f32x16 dp_prev = zero16();
+  // role 0, step t: rows [i, i + 32)
+  auto p_step = [&](int t, int at, int i) __attribute__((always_inline)) {
+    Frag f[KS];
+    rows_of(buf[at], f);
+    const f32x16 lse = stats16(at);
+    __builtin_amdgcn_sched_barrier(0);
+    f32x16 sc = product(f, zero16());
+    bf16x8 tf[MB];
+    first_half(buf[at] + T32, tf);
+    __builtin_amdgcn_sched_barrier(0);
+    if (i < from_last || i + kTile > s.nq) {        // (rows behind the last one were loaded as zeros, their statistics too)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int r = i + 8 * (e >> 2) + 4 * kg + (e & 3);
+        if (r < from || r >= s.nq) sc[e] = -INFINITY;
+      }
+    }
+    bf16x8 pf[2];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) pf[e >> 3][e & 7] = (__bf16)__builtin_amdgcn_exp2f(fmaf(sc[e], a.c, -lse[e]));
+    ph[t & 1][rh][0][lane] = __builtin_bit_cast(u32x4, pf[0]);
+    ph[t & 1][rh][1][lane] = __builtin_bit_cast(u32x4, pf[1]);
+    accumulate(buf[at] + T32, tf, pf);
+  };
+  auto ds_finish = [&](int at, const u32x4 (&pu)[2], const bf16x8 (&tf)[MB]) __attribute__((always_inline)) {
+    bf16x8 ds[2];
+    const bf16x8 pf[2] = {__builtin_bit_cast(bf16x8, pu[0]), __builtin_bit_cast(bf16x8, pu[1])};
+#pragma unroll
+    for (int e = 0; e < 16; ++e) ds[e >> 3][e & 7] = (__bf16)((float)pf[e >> 3][e & 7] * dp_prev[e]);
+    accumulate(buf[at], tf, ds);
+  };
+  auto take_p = [&](int t, u32x4 (&pu)[2]) __attribute__((always_inline)) {
+    pu[0] = ph[t & 1][rh][0][lane];
+    pu[1] = ph[t & 1][rh][1][lane];
+  };
+  const int steps = steps_all * a.G;
+  int wi = i_first;                 // rows of the present step
+  if (steps > 0) {
+    request(0);
+    __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+    lds_barrier();
+    if (steps > 1) request(1);
+    if (!is_ds) {
+      p_step(0, 0, wi);
+    } else {
+      Frag f[KS];
+      dp_prev = stats16(0);
+      rows_of(buf[0] + T32, f);
+      dp_prev = product(f, dp_prev);
+    }
+    auto step = [&](int t, int cur, int nxt, int prv) __attribute__((always_inline)) {
+      wi += kTile;
+      if (wi >= s.nq) wi = i_first;
+      __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+      lds_barrier();
+      if (t + 1 < steps) request(nxt);
+      if (!is_ds) {
+        p_step(t, cur, wi);
+      } else {
+        Frag f[KS];
+        u32x4 pu[2];
+        f32x16 dp_cur = stats16(cur);
+        rows_of(buf[cur] + T32, f);
+        take_p(t - 1, pu);
+        __builtin_amdgcn_sched_barrier(0);
+        dp_cur = product(f, dp_cur);
+        bf16x8 tf[MB];
+        first_half(buf[prv], tf);
+        __builtin_amdgcn_sched_barrier(0);
+        ds_finish(prv, pu, tf);
+        dp_prev = dp_cur;
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    for (int t = 1; t < steps; t += 3) {
+      step(t, 1, 2, 0);
+      if (t + 1 >= steps) break;
+      step(t + 1, 2, 0, 1);
+      if (t + 2 >= steps) break;
+      step(t + 2, 0, 1, 2);
+    }
+    lds_barrier();
+    if (is_ds) {
+      u32x4 pu[2];
+      bf16x8 tf[MB];
+      const int prv = (steps - 1) % 3;
+      take_p(steps - 1, pu);
+      first_half(buf[prv], tf);
+      ds_finish(prv, pu, tf);
+    }
+  }
+  if (!ok) return;
+  uint16_t* op = is_ds ? a.dK + (int64_t)hk * a.k_head + token * a.k_tok : a.dV + (int64_t)hk * a.v_head + token * a.v_tok;
+  const float factor = is_ds ? a.scale : 1.0f;
+#pragma unroll
+  for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      bf16x4 o4;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o4[e] = (__bf16)(acc[mb][4 * g + e] * factor);
+      *reinterpret_cast<bf16x4*>(op + 32 * mb + 8 * g + 4 * kg) = o4;
+    }
+}
+
+template <int D> int launch(const PackedArgs& a, hipStream_t st) {
+  if (a.q_len > 0) {
+    const int64_t rows = (int64_t)a.H * a.q_len;
+    if (lf_launch(lf_packed_delta_kernel<D>, dim3((unsigned)((rows - 1) / (256 / (D / 8)) + 1)), dim3(256), 0, st, a) != hipSuccess) return LF_ERR_HIP;
+    const int64_t tiles = (int64_t)(a.q_len / 128 + a.seqs) * a.H;
+    PackedArgs q = a;
+    q.slots = a.q_len / 128 + a.seqs;
+    if (lf_launch(lf_packed_dq_kernel<D>, dim3((unsigned)tiles), dim3(256), 0, st, q) != hipSuccess) return LF_ERR_HIP;
+  }
+  if (a.kv_len == 0) return LF_OK;
+  return lf_launch(lf_packed_dkv_kernel<D>, dim3((unsigned)((int64_t)(a.kv_len / 64 + a.seqs) * a.Hk)), dim3(256), 0, st, a) == hipSuccess ? LF_OK : LF_ERR_HIP;
+}
+
+}  // namespace
+
+int lf_launch_packed_bwd(const lf_packed_call* c, void* stream) {
+  PackedArgs a = lf_packed_args(c);
+  a.ndelta = (float*)c->workspace;
+  a.parts = 1;
+  return c->s->head_dim == 128 ? launch<128>(a, (hipStream_t)stream) : launch<64>(a, (hipStream_t)stream);
+}

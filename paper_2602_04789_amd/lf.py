@@ -15,7 +15,8 @@ _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "liblf_hsa.
 _lib = None
 
 LF_OK = 0
-LF_BF16 = 0
+LF_BF16, LF_F32 = 0, 1
+LF_NORM_LAYER, LF_NORM_RMS = 0, 1
 LF_SCHED_FIXED, LF_SCHED_LINEAR, LF_SCHED_CAG = 0, 1, 2
 LF_OF_CANDIDATES, LF_OF_HISTORY, LF_OF_ALL = 0, 1, 2
 
@@ -79,6 +80,26 @@ class lf_token_shape(C.Structure):
                 ("k_stride_tok", C.c_int64), ("k_stride_head", C.c_int64),
                 ("v_stride_tok", C.c_int64), ("v_stride_head", C.c_int64),
                 ("o_stride_tok", C.c_int64), ("o_stride_head", C.c_int64)]
+
+
+class lf_norm_shape(C.Structure):
+    _fields_ = [("tokens", C.c_int32), ("channels", C.c_int32), ("groups", C.c_int32), ("group_len", C.c_int32),
+                ("stream_dtype", C.c_int32), ("kind", C.c_int32), ("eps", C.c_float), ("residual_scale", C.c_float),
+                ("x_stride", C.c_int64), ("xo_stride", C.c_int64), ("b_stride", C.c_int64), ("y_stride", C.c_int64),
+                ("gate_stride", C.c_int64), ("scale_stride", C.c_int64), ("shift_stride", C.c_int64)]
+
+
+class lf_packed_shape(C.Structure):
+    _fields_ = [("heads", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("seqs", C.c_int32),
+                ("q_len", C.c_int32), ("kv_len", C.c_int32), ("causal", C.c_int32), ("dtype", C.c_int32),
+                ("q_stride_tok", C.c_int64), ("q_stride_head", C.c_int64),
+                ("k_stride_tok", C.c_int64), ("k_stride_head", C.c_int64),
+                ("v_stride_tok", C.c_int64), ("v_stride_head", C.c_int64),
+                ("o_stride_tok", C.c_int64), ("o_stride_head", C.c_int64)]
+
+
+class lf_grad_tensor(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("out", C.c_void_p), ("numel", C.c_int64), ("dtype", C.c_int32), ("out_dtype", C.c_int32)]
 
 
 class LfError(RuntimeError):
@@ -152,6 +173,25 @@ def load() -> C.CDLL:
     lib.lf_token_attn_kvq_workspace_bytes.restype = C.c_size_t
     lib.lf_token_attn_kvq.argtypes = [vp, vp, C.c_size_t, kvp, vp, vp, tkp, C.c_float, vp, vp, C.c_size_t, vp]
     lib.lf_token_attn_kvq.restype = C.c_int
+    nrp, pkp = C.POINTER(lf_norm_shape), C.POINTER(lf_packed_shape)
+    lib.lf_gate_norm.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, nrp, vp, vp, vp]
+    lib.lf_gate_norm.restype = C.c_int
+    lib.lf_gate_norm_bwd_workspace_bytes.argtypes = [nrp]
+    lib.lf_gate_norm_bwd_workspace_bytes.restype = C.c_size_t
+    lib.lf_gate_norm_bwd.argtypes = [vp, vp, vp, vp, vp, vp, vp, nrp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, C.c_size_t, vp]
+    lib.lf_gate_norm_bwd.restype = C.c_int
+    lib.lf_packed_attn_workspace_bytes.argtypes = [pkp]
+    lib.lf_packed_attn_workspace_bytes.restype = C.c_size_t
+    lib.lf_packed_attn.argtypes = [vp, vp, vp, pkp, vp, vp, C.c_float, vp, vp, vp, C.c_size_t, vp]
+    lib.lf_packed_attn.restype = C.c_int
+    lib.lf_packed_attn_bwd_workspace_bytes.argtypes = [pkp]
+    lib.lf_packed_attn_bwd_workspace_bytes.restype = C.c_size_t
+    lib.lf_packed_attn_bwd.argtypes = [vp, vp, vp, vp, vp, vp, pkp, vp, vp, C.c_float, vp, vp, vp, vp, C.c_size_t, vp]
+    lib.lf_packed_attn_bwd.restype = C.c_int
+    lib.lf_grad_workspace_bytes.argtypes = [C.c_int32, C.c_int64]
+    lib.lf_grad_workspace_bytes.restype = C.c_size_t
+    lib.lf_grad_clip.argtypes = [vp, C.c_int32, C.c_float, C.c_float, vp, vp, C.c_size_t, vp]
+    lib.lf_grad_clip.restype = C.c_int
     lib.lf_kcache_bytes.argtypes = [C.POINTER(lf_shape), C.c_int32]
     lib.lf_kcache_bytes.restype = C.c_size_t
     lib.lf_kcache_update.argtypes = [vp, C.POINTER(lf_shape), C.c_int32, C.c_int32, C.c_int32, vp,
@@ -799,3 +839,274 @@ def lf_token_attn_kvq(Q, cache, capacity: int, cached_len: int, K=None, V=None, 
     if rc != LF_OK:
         raise LfError(rc, "lf_token_attn_kvq")
     return O
+
+
+_stream_dtypes = None      # torch type -> lf_dtype, for streams and gradients
+
+
+def _dtype_of(t, name: str) -> int:
+    global _stream_dtypes
+    if _stream_dtypes is None:
+        torch = _torch or _get_torch()
+        _stream_dtypes = {torch.bfloat16: LF_BF16, torch.float32: LF_F32}
+    try:
+        return _stream_dtypes[t.dtype]
+    except KeyError:
+        raise ValueError(f"{name} must be bfloat16 or float32") from None
+
+
+def _row_stride(t, shape, dtype, name: str) -> int:
+    """Row stride of a [L, C] tensor with contiguous channels; that of a single row does not matter."""
+    st = t.stride()
+    if t.shape != shape or len(st) != 2 or t.dtype is not dtype or (st[1] != 1 and shape[1] != 1):
+        raise ValueError(f"{name} must be {dtype} {list(shape)} with contiguous channels")
+    return st[0] if shape[0] != 1 else shape[1]
+
+
+def _norm_call(L, C_, dtype, kind, eps, residual_scale, gate, post_weight, weight, scale, shift, starts, group_len):
+    """(shape of the call, its groups); the row strides are still to be set."""
+    torch = _torch or _get_torch()
+    f32 = torch.float32
+    group_len, kind = _int32(group_len, kind)
+    if (starts is None) == (group_len <= 0):
+        raise ValueError("groups are given by group_len > 0 or by starts")
+    if starts is not None:
+        if starts.dtype is not torch.int32 or starts.dim() != 1 or not starts.is_contiguous() or starts.shape[0] < 2:
+            raise ValueError("starts must be contiguous int32 [groups + 1]")
+        groups = starts.shape[0] - 1
+    else:
+        groups = -(-L // group_len)
+    for t, name in ((post_weight, "post_weight"), (weight, "weight")):
+        if t is not None and (t.dtype is not f32 or t.shape != (C_,) or not t.is_contiguous()):
+            raise ValueError(f"{name} must be contiguous float32 [channels]")
+    strides = [C_ if t is None else _row_stride(t, (groups, C_), f32, name)
+               for t, name in ((gate, "gate"), (scale, "scale"), (shift, "shift"))]
+    return lf_norm_shape(L, C_, groups, group_len, dtype, kind, float(eps), float(residual_scale), C_, C_, C_, C_, *strides), groups
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def lf_gate_norm(X, B=None, gate=None, post_weight=None, weight=None, scale=None, shift=None, group_len: int = 0, starts=None,
+                 kind: int = LF_NORM_LAYER, eps: float = 1e-6, residual_scale: float = 1.0, Xout=None, Y=None, stream=None):
+    """Between two blocks: Xout = X + residual_scale * gate * (B, or its RMSNorm with ``post_weight``) and Y = norm(Xout) * weight * (1 + scale) +
+    shift; returns (Xout, Y).  X [L, C] bfloat16 or float32, B [L, C] and Y bfloat16; gate, scale and shift float32 [groups, C], one row for ``group_len``
+    tokens or for the tokens [starts[g], starts[g + 1]) (int32, device); without B, Xout is X.  Xout may be X itself."""
+    torch = _torch or _get_torch()
+    if X.dim() != 2:
+        raise ValueError("X must be [L, C]")
+    L, C_ = X.shape
+    p, _ = _norm_call(L, C_, _dtype_of(X, "X"), kind, eps, residual_scale, gate, post_weight, weight, scale, shift, starts, group_len)
+    at, st = _here(stream)
+    p.x_stride = _row_stride(X, (L, C_), X.dtype, "X")
+    if B is not None:
+        p.b_stride = _row_stride(B, (L, C_), torch.bfloat16, "B")
+        if Xout is None:
+            Xout = _new(stream, X.new_empty, (L, C_))
+        p.xo_stride = _row_stride(Xout, (L, C_), X.dtype, "Xout")
+    elif gate is not None or post_weight is not None or Xout is not None:
+        raise ValueError("gate, post_weight and Xout go with B")
+    if Y is None:
+        Y = _new(stream, X.new_empty, (L, C_), dtype=torch.bfloat16)
+    p.y_stride = _row_stride(Y, (L, C_), torch.bfloat16, "Y")
+    _one_device(at, [t for t in (X, B, gate, post_weight, weight, scale, shift, starts, Xout, Y) if t is not None])
+    rc = (_lib or load()).lf_gate_norm(X.data_ptr(), _ptr(B), _ptr(gate), _ptr(post_weight), _ptr(weight), _ptr(scale), _ptr(shift), _ptr(starts),
+                                       C.byref(p), _ptr(Xout), Y.data_ptr(), st)
+    if rc != LF_OK:
+        raise LfError(rc, "lf_gate_norm")
+    return (X if B is None else Xout), Y
+
+
+def lf_gate_norm_bwd_workspace_bytes(tokens: int, channels: int, groups: int, group_len: int = 0) -> int:
+    """Scratch of one call (0 on bad input); group_len = 0: groups are given by ``starts``."""
+    return _size_of(load().lf_gate_norm_bwd_workspace_bytes,
+                    lambda L, c, g, n: (lf_norm_shape(L, c, g, n, LF_BF16, LF_NORM_LAYER, 0.0, 1.0, c, c, c, c, c, c, c),), tokens, channels, groups,
+                    group_len)
+
+
+def lf_gate_norm_bwd(Xout, dY, dXout=None, B=None, gate=None, post_weight=None, weight=None, scale=None, group_len: int = 0, starts=None,
+                     kind: int = LF_NORM_LAYER, eps: float = 1e-6, residual_scale: float = 1.0, dX=None, dB=None, workspace=None, stream=None):
+    """Gradients of lf_gate_norm for upstream gradients dY of Y (may be None: zeros) and dXout of Xout (likewise); Xout as the forward call returned it.
+    Returns (dX, dB, dgate, dpost_weight, dweight, dscale, dshift): dX with the type of the stream (``dX`` may be dXout itself), dB bfloat16,
+    the tables' gradients float32 [groups, C] and [C], None for what the call does not have (dscale and dshift are always there)."""
+    torch = _torch or _get_torch()
+    bf, f32 = torch.bfloat16, torch.float32
+    if Xout.dim() != 2:
+        raise ValueError("Xout must be [L, C]")
+    L, C_ = Xout.shape
+    p, groups = _norm_call(L, C_, _dtype_of(Xout, "Xout"), kind, eps, residual_scale, gate, post_weight, weight, scale, None, starts, group_len)
+    at, st = _here(stream)
+    p.xo_stride = _row_stride(Xout, (L, C_), Xout.dtype, "Xout")
+    if dY is not None:
+        p.y_stride = _row_stride(dY, (L, C_), bf, "dY")
+    if dXout is not None and _row_stride(dXout, (L, C_), Xout.dtype, "dXout") != p.xo_stride:
+        raise ValueError("dXout must have the strides of Xout")
+    if dX is None:
+        dX = _new(stream, torch.empty_strided, (L, C_), (p.xo_stride, 1), dtype=Xout.dtype, device=Xout.device)
+    if _row_stride(dX, (L, C_), Xout.dtype, "dX") != p.xo_stride:
+        raise ValueError("dX must have the strides of Xout")
+    if B is not None:
+        p.b_stride = _row_stride(B, (L, C_), bf, "B")
+        if dB is None:
+            dB = _new(stream, torch.empty_strided, (L, C_), (p.b_stride, 1), dtype=bf, device=B.device)
+        if _row_stride(dB, (L, C_), bf, "dB") != p.b_stride:
+            raise ValueError("dB must have the strides of B")
+    elif gate is not None or post_weight is not None or dB is not None:
+        raise ValueError("gate, post_weight and dB go with B")
+    _one_device(at, [t for t in (Xout, dY, dXout, B, gate, post_weight, weight, scale, starts, dX, dB) if t is not None])
+    new = lambda there, *shape: _new(stream, Xout.new_empty, shape, dtype=f32) if there else None
+    dgate, dscale, dshift = new(gate is not None, groups, C_), new(True, groups, C_), new(True, groups, C_)
+    dpost, dweight = new(post_weight is not None, C_), new(weight is not None, C_)
+    lib = _lib or load()
+    ws = _workspace(workspace, lambda: lib.lf_gate_norm_bwd_workspace_bytes(C.byref(p)), Xout, stream, at)
+    rc = lib.lf_gate_norm_bwd(Xout.data_ptr(), _ptr(B), _ptr(gate), _ptr(post_weight), _ptr(weight), _ptr(scale), _ptr(starts), C.byref(p), _ptr(dY),
+                              _ptr(dXout), dX.data_ptr(), _ptr(dB), _ptr(dgate), _ptr(dpost), _ptr(dweight), _ptr(dscale), _ptr(dshift),
+                              *_bytes_of(ws), st)
+    if rc != LF_OK:
+        raise LfError(rc, "lf_gate_norm_bwd")
+    return dX, dB, dgate, dpost, dweight, dscale, dshift
+
+
+def _packed(Q, K, V, O, q_start, kv_start, causal):
+    """(shape of the call, its tensors) for [H, L, d] tensors."""
+    torch = _torch or _get_torch()
+    (qsh, qt, qh), (ksh, kt, kh), (vsh, vt, vh), (osh, ot, oh) = _rows(Q, "Q"), _rows(K, "K"), _rows(V, "V"), _rows(O, "O")
+    if ksh != vsh or ksh[2] != qsh[2] or osh != qsh:
+        raise ValueError("K and V must be [kv_heads, kv_len, d], O [heads, q_len, d] as Q")
+    for t, name in ((q_start, "q_start"), (kv_start, "kv_start")):
+        if t.dtype is not torch.int32 or t.dim() != 1 or not t.is_contiguous() or t.shape[0] < 2:
+            raise ValueError(f"{name} must be contiguous int32 [seqs + 1]")
+    if q_start.shape != kv_start.shape:
+        raise ValueError("q_start and kv_start must have one length")
+    causal, q_len, kv_len = _int32(causal, qsh[1], ksh[1])
+    return lf_packed_shape(qsh[0], ksh[0], qsh[2], q_start.shape[0] - 1, q_len, kv_len, causal, LF_BF16, qt, qh, kt, kh, vt, vh, ot, oh)
+
+
+def _packed_sizes(query, heads, kv_heads, head_dim, seqs, q_len, kv_len, causal) -> int:
+    return _size_of(query, lambda H, Hk, d, b, q, kv, u: (lf_packed_shape(H, Hk, d, b, q, kv, u, LF_BF16, d, 0, d, 0, d, 0, d, 0),),
+                    heads, kv_heads, head_dim, seqs, q_len, kv_len, causal)
+
+
+def lf_packed_attn_workspace_bytes(heads: int, kv_heads: int, head_dim: int, seqs: int, q_len: int, kv_len: int, causal: int = 0) -> int:
+    """Scratch of one forward call (0 on bad input too); q_len and kv_len are the tensors' rows, of all sequences."""
+    return _packed_sizes(load().lf_packed_attn_workspace_bytes, heads, kv_heads, head_dim, seqs, q_len, kv_len, causal)
+
+
+def _packed_fwd(Q, K, V, q_start, kv_start, causal, softmax_scale, O, lse2, with_lse, workspace, stream, where):
+    torch = _torch or _get_torch()
+    at, st = _here(stream)
+    if O is None:
+        O = _new(stream, Q.new_empty, Q.shape)
+    p = _packed(Q, K, V, O, q_start, kv_start, causal)
+    if with_lse:
+        if lse2 is None:
+            lse2 = _new(stream, Q.new_empty, Q.shape[:2], dtype=torch.float32)
+        if lse2.dtype is not torch.float32 or lse2.shape != Q.shape[:2] or not lse2.is_contiguous():
+            raise ValueError("lse2 must be a contiguous float32 GPU tensor [heads, q_len]")
+        _one_device(at, (Q, K, V, O, q_start, kv_start, lse2))
+    else:
+        _one_device(at, (Q, K, V, O, q_start, kv_start))
+    lib = _lib or load()
+    ws = _workspace(workspace, lambda: lib.lf_packed_attn_workspace_bytes(C.byref(p)), Q, stream, at)
+    rc = lib.lf_packed_attn(Q.data_ptr(), K.data_ptr(), V.data_ptr(), C.byref(p), q_start.data_ptr(), kv_start.data_ptr(), float(softmax_scale),
+                            O.data_ptr(), _ptr(lse2), *_bytes_of(ws), st)
+    if rc != LF_OK:
+        raise LfError(rc, where)
+    return O, lse2
+
+
+def lf_packed_attn(Q, K, V, q_start, kv_start, causal: int = 0, softmax_scale: float = 0.0, O=None, workspace=None, stream=None):
+    """Attention over packed sequences: Q [heads, q_len, d], K and V [kv_heads, kv_len, d] (bfloat16), sequence b with the rows
+    [q_start[b], q_start[b + 1]) and the tokens [kv_start[b], kv_start[b + 1]) (int32, device).  ``causal`` 0: rows see their whole sequence, 1: the
+    tokens up to their own (the last row the last token), u: up to the end of their chunk of u.  Returns O; rows of no sequence are left as they are
+    (those of a new tensor hold anything)."""
+    return _packed_fwd(Q, K, V, q_start, kv_start, causal, softmax_scale, O, None, False, workspace, stream, "lf_packed_attn")[0]
+
+
+def lf_packed_attn_fwd(Q, K, V, q_start, kv_start, causal: int = 0, softmax_scale: float = 0.0, O=None, lse2=None, workspace=None, stream=None):
+    """lf_packed_attn that also leaves the rows' log-sum-exp (exp2 domain, float32 [heads, q_len]) for lf_packed_attn_bwd; returns (O, lse2)."""
+    return _packed_fwd(Q, K, V, q_start, kv_start, causal, softmax_scale, O, lse2, True, workspace, stream, "lf_packed_attn_fwd")
+
+
+def lf_packed_attn_bwd_workspace_bytes(heads: int, kv_heads: int, head_dim: int, seqs: int, q_len: int, kv_len: int, causal: int = 0) -> int:
+    return _packed_sizes(load().lf_packed_attn_bwd_workspace_bytes, heads, kv_heads, head_dim, seqs, q_len, kv_len, causal)
+
+
+def lf_packed_attn_bwd(Q, K, V, O, dO, lse2, q_start, kv_start, causal: int = 0, softmax_scale: float = 0.0, workspace=None, stream=None, grads=None):
+    """Gradients of lf_packed_attn_fwd; returns (dQ, dK, dV), bfloat16 with the strides of Q, K and V (``grads``: three such tensors to write into).
+    Rows and tokens of no sequence are left as they are (those of new tensors hold anything)."""
+    torch = _torch or _get_torch()
+    at, st = _here(stream)
+    p = _packed(Q, K, V, O, q_start, kv_start, causal)
+    if _rows(dO, "dO")[0] != O.shape or (dO.stride() != O.stride() and _rows(dO, "dO")[1:] != (p.o_stride_tok, p.o_stride_head)):
+        raise ValueError("dO must have the shape and strides of O")
+    if lse2.dtype is not torch.float32 or lse2.shape != Q.shape[:2] or not lse2.is_contiguous():
+        raise ValueError("lse2 must be a contiguous float32 GPU tensor [heads, q_len]")
+    if grads is None:
+        grads = [_new(stream, torch.empty_strided, t.shape, t.stride(), dtype=t.dtype, device=t.device) for t in (Q, K, V)]
+    else:
+        for g, t, name in zip(grads, (Q, K, V), ("dQ", "dK", "dV")):
+            if g.shape != t.shape or _rows(g, name)[1:] != _rows(t, name)[1:]:
+                raise ValueError(f"{name} must have the shape and strides of its input")
+    dQ, dK, dV = grads
+    _one_device(at, (Q, K, V, O, dO, lse2, q_start, kv_start, dQ, dK, dV))
+    lib = _lib or load()
+    ws = _workspace(workspace, lambda: lib.lf_packed_attn_bwd_workspace_bytes(C.byref(p)), Q, stream, at)
+    rc = lib.lf_packed_attn_bwd(Q.data_ptr(), K.data_ptr(), V.data_ptr(), O.data_ptr(), dO.data_ptr(), lse2.data_ptr(), C.byref(p), q_start.data_ptr(),
+                                kv_start.data_ptr(), float(softmax_scale), dQ.data_ptr(), dK.data_ptr(), dV.data_ptr(), *_bytes_of(ws), st)
+    if rc != LF_OK:
+        raise LfError(rc, "lf_packed_attn_bwd")
+    return dQ, dK, dV
+
+
+def lf_grad_workspace_bytes(count: int, numel: int) -> int:
+    """Scratch of lf_grad_clip for `count` tensors of `numel` elements in all (0 on bad input)."""
+    try:
+        count, = _int32(count)
+    except ValueError:
+        return 0
+    return int(load().lf_grad_workspace_bytes(count, numel)) if 0 <= numel <= 1 << 40 else 0
+
+
+def lf_grad_clip(grads, max_norm: float, out=None, eps: float = 1e-6, norm=None, workspace=None, stream=None):
+    """Scales gradients to a largest norm: x * min(1, max_norm / (norm + eps)), in place or into the tensors of ``out`` (one for each, of the
+    same size; bfloat16 or float32), and returns the norm over all of them, float32 [1] on the device.  Where that is not finite they are not scaled;
+    max_norm = inf takes the norm alone.  ``grads``: tensors of bfloat16 or float32 without holes."""
+    torch = _torch or _get_torch()
+    grads = list(grads)
+    to = grads if out is None else list(out)
+    if len(to) != len(grads):
+        raise ValueError("out must have a tensor for each gradient")
+    at, st = _here(stream)
+    table, total = (lf_grad_tensor * max(len(grads), 1))(), 0
+    for i, (x, y) in enumerate(zip(grads, to)):
+        n = x.numel()
+        if x.get_device() != at or y.get_device() != at:
+            raise ValueError("all tensors must live on the current device")
+        if not x.is_contiguous() and not (x is y and _dense(x)):
+            raise ValueError("gradients must be contiguous (in place: without holes)")
+        if x is not y and (y.numel() != n or not y.is_contiguous()):
+            raise ValueError("out must be contiguous tensors of their gradients' sizes")
+        table[i] = lf_grad_tensor(x.data_ptr(), None if x is y else y.data_ptr(), n, _dtype_of(x, "a gradient"), _dtype_of(y, "out"))
+        total += n
+    if norm is None:
+        norm = _new(stream, torch.empty, (1,), dtype=torch.float32, device=torch.device("cuda", at))
+    if norm.dtype is not torch.float32 or norm.numel() != 1 or norm.get_device() != at:
+        raise ValueError("norm must be one float32 on the current device")
+    lib = _lib or load()
+    ws = _workspace(workspace, lambda: lib.lf_grad_workspace_bytes(len(grads), total), norm, stream, at)
+    rc = lib.lf_grad_clip(table, len(grads), float(max_norm), float(eps), norm.data_ptr(), *_bytes_of(ws), st)
+    if rc != LF_OK:
+        raise LfError(rc, "lf_grad_clip")
+    return norm
+
+
+def _dense(t) -> bool:
+    """Whether the elements of a tensor fill their memory without holes or overlaps, in whatever order."""
+    want = 1
+    for st, n in sorted((st, n) for st, n in zip(t.stride(), t.shape) if n != 1):
+        if st != want:
+            return False
+        want *= n
+    return True
