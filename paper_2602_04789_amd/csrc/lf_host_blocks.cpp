@@ -77,8 +77,6 @@ int check_sizes(const lf_packed_shape* s) {
   const int64_t dq = ((int64_t)s->q_len / 128 + s->seqs) * s->heads, dkv = ((int64_t)s->kv_len / 64 + s->seqs) * s->kv_heads;
   if (dq > blocks) blocks = dq;
   if (dkv > blocks) blocks = dkv;
-  const int64_t delta = (int64_t)s->heads * s->q_len / (256 / (s->head_dim / 8)) + 1;
-  if (delta > blocks) blocks = delta;
   return blocks * 256 < kMostThreads ? LF_OK : LF_ERR_SHAPE;
 }
 int check_packed(const lf_packed_shape* s) {

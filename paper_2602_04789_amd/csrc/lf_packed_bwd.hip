@@ -18,29 +18,13 @@ template <int CH> __device__ __forceinline__ int both_swz(int row, int ch) {
 }
 template <int CH> constexpr int kTrHiFlip = CH == 16 ? 16 : 0;
 
-// -delta of every row of every sequence: CH lanes a row.
-template <int D>
-__global__ __launch_bounds__(256) void lf_packed_delta_kernel(PackedArgs a) {
-  constexpr int CH = D / 8;
-  const int64_t x = (int64_t)blockIdx.x * (256 / CH) + threadIdx.x / CH;
-  if (x >= (int64_t)a.H * a.q_len) return;
-  const int h = (int)(x / a.q_len), ch = threadIdx.x % CH;
-  const int64_t i = x % a.q_len;
-  const int64_t at = (int64_t)h * a.o_head + i * a.o_tok + 8 * ch;
-  const u32x4 o = *reinterpret_cast<const u32x4*>(a.O + at), g = *reinterpret_cast<const u32x4*>(a.dO + at);
-  float v = 0.0f;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    v = fmaf(__uint_as_float(o[e] << 16), __uint_as_float(g[e] << 16), v);
-    v = fmaf(__uint_as_float(o[e] & 0xffff0000u), __uint_as_float(g[e] & 0xffff0000u), v);
-  }
-#pragma unroll
-  for (int off = 1; off < CH; off <<= 1) v += __shfl_xor(v, off);
-  if (ch == 0) a.ndelta[x] = -v;
-}
+// Rows that see this many tokens or fewer get delta = sum_y P dP (the same number) instead of dO . O: O was rounded to bfloat16, and where few
+// tokens share a row's probability, one of them nearly all of it, what that leaves in dP - delta is more than the roundings of P and dS (12
+// sequences of one to four tokens: dQ off by 4.8e-3 in the 2-norm).
+constexpr int kShort = 256;
 
-// dQ: four wavefronts of 32 rows each share tiles of 32 tokens of K and V.
-template <int D>
+// dQ: four wavefronts of 32 rows each share tiles of 32 tokens of K and V.  DELTA: the launch before it, -delta of every row.
+template <int D, bool DELTA>
 __global__ __launch_bounds__(256, 2) void lf_packed_dq_kernel(PackedArgs a) {
   constexpr int kRows = 128;
   constexpr int CH = D / 8, KS = D / 16, MB = D / 32;
@@ -64,11 +48,13 @@ __global__ __launch_bounds__(256, 2) void lf_packed_dq_kernel(PackedArgs a) {
   const int row = 32 * wave + ln;
   const bool ok = row < rows;
   const int64_t token = (int64_t)s.q0 + i0 + row;
-  const int lim = row_limit(s, a.unit, min(i0 + row, s.nq - 1));
+  // A row that sees a single token has no gradient of its scores: P = 1 whatever they are.
+  int lim = row_limit(s, a.unit, min(i0 + row, s.nq - 1));
+  if (lim == 1) lim = 0;
   const bool active = 32 * wave < rows;
-  const int lim_first = row_limit(s, a.unit, i0 + 32 * wave);
+  const int lim_first = s.nk == 1 || row_limit(s, a.unit, i0 + 32 * wave) <= 1 ? 0 : row_limit(s, a.unit, i0 + 32 * wave);
   const int lim_last = active ? row_limit(s, a.unit, i0 + min(32 * wave + 31, rows - 1)) : 0;
-  const int seen = row_limit(s, a.unit, i0 + rows - 1);
+  const int seen_all = row_limit(s, a.unit, i0 + rows - 1), seen = DELTA && seen_all > kShort ? 0 : seen_all;
 
   Frag qf[KS], gf[KS];
 #pragma unroll
@@ -79,10 +65,10 @@ __global__ __launch_bounds__(256, 2) void lf_packed_dq_kernel(PackedArgs a) {
       gf[k].u = *reinterpret_cast<const u32x4*>(a.dO + (int64_t)h * a.o_head + token * a.o_tok + 16 * k + 8 * kg);
     }
   }
-  float lse = INFINITY, nd = 0.0f;
+  float lse = INFINITY, nd = 0.0f, delta = 0.0f;
   if (ok) {
     lse = a.lse2[(int64_t)h * a.q_len + token];
-    nd = a.ndelta[(int64_t)h * a.q_len + token];
+    if constexpr (!DELTA) nd = a.ndelta[(int64_t)h * a.q_len + token];
   }
   const uint16_t* Kh = a.K + (int64_t)hk * a.k_head;
   const uint16_t* Vh = a.V + (int64_t)hk * a.v_head;
@@ -137,6 +123,11 @@ __global__ __launch_bounds__(256, 2) void lf_packed_dq_kernel(PackedArgs a) {
       for (int i = 0; i < 16; ++i)
         if (t + 8 * (i >> 2) + 4 * kg + (i & 3) >= lim) sc[i] = -INFINITY;
     }
+    if constexpr (DELTA) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) delta = fmaf(__builtin_amdgcn_exp2f(fmaf(sc[i], a.c, -lse)), dp[i], delta);
+      return;
+    }
     bf16x8 ds[2];
 #pragma unroll
     for (int i = 0; i < 16; ++i) ds[i >> 3][i & 7] = (__bf16)(__builtin_amdgcn_exp2f(fmaf(sc[i], a.c, -lse)) * dp[i]);
@@ -157,6 +148,22 @@ __global__ __launch_bounds__(256, 2) void lf_packed_dq_kernel(PackedArgs a) {
     lds_barrier();
     if (t + kTile < seen) request(t + kTile, stage[cur ^ 1]);
     if (t < lim_last) work(t, stage[cur]);
+  }
+  if constexpr (DELTA) {
+    if (seen_all > kShort && ok) {
+#pragma unroll
+      for (int k = 0; k < KS; ++k) {
+        const u32x4 o = *reinterpret_cast<const u32x4*>(a.O + (int64_t)h * a.o_head + token * a.o_tok + 16 * k + 8 * kg);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          delta = fmaf(__uint_as_float(o[e] << 16), __uint_as_float(gf[k].u[e] << 16), delta);
+          delta = fmaf(__uint_as_float(o[e] & 0xffff0000u), __uint_as_float(gf[k].u[e] & 0xffff0000u), delta);
+        }
+      }
+    }
+    delta += __shfl_xor(delta, 32);
+    if (ok && kg == 0) a.ndelta[(int64_t)h * a.q_len + token] = -delta;
+    return;
   }
   if (!ok) return;
   uint16_t* op = a.dQ + (int64_t)h * a.q_head + token * a.q_tok;
@@ -316,8 +323,15 @@ __global__ __launch_bounds__(256, 2) void lf_packed_dkv_kernel(PackedArgs a) {
     ph[t & 1][rh][1][lane] = __builtin_bit_cast(u32x4, pf[1]);
     accumulate(buf[at] + T32, tf, pf);
   };
-  auto ds_finish = [&](int at, const u32x4 (&pu)[2], const bf16x8 (&tf)[MB]) __attribute__((always_inline)) {
+  // the one row that sees a single token (all rows of a sequence of one token do): see the dQ kernel
+  const int lone = a.unit == 1 ? s.nq - s.nk : -1;
+  auto ds_finish = [&](int at, int i, const u32x4 (&pu)[2], const bf16x8 (&tf)[MB]) __attribute__((always_inline)) {
     bf16x8 ds[2];
+    if (s.nk == 1 || (lone >= i && lone < i + kTile)) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        if (s.nk == 1 || i + 8 * (e >> 2) + 4 * kg + (e & 3) == lone) dp_prev[e] = 0.0f;
+    }
     const bf16x8 pf[2] = {__builtin_bit_cast(bf16x8, pu[0]), __builtin_bit_cast(bf16x8, pu[1])};
 #pragma unroll
     for (int e = 0; e < 16; ++e) ds[e >> 3][e & 7] = (__bf16)((float)pf[e >> 3][e & 7] * dp_prev[e]);
@@ -328,7 +342,7 @@ __global__ __launch_bounds__(256, 2) void lf_packed_dkv_kernel(PackedArgs a) {
     pu[1] = ph[t & 1][rh][1][lane];
   };
   const int steps = steps_all * a.G;
-  int wi = i_first;                 // rows of the present step
+  int wi = i_first, wp = i_first;   // rows of the present step, and of the one before
   if (steps > 0) {
     request(0);
     __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
@@ -343,6 +357,7 @@ __global__ __launch_bounds__(256, 2) void lf_packed_dkv_kernel(PackedArgs a) {
       dp_prev = product(f, dp_prev);
     }
     auto step = [&](int t, int cur, int nxt, int prv) __attribute__((always_inline)) {
+      wp = wi;
       wi += kTile;
       if (wi >= s.nq) wi = i_first;
       __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
@@ -361,7 +376,7 @@ __global__ __launch_bounds__(256, 2) void lf_packed_dkv_kernel(PackedArgs a) {
         bf16x8 tf[MB];
         first_half(buf[prv], tf);
         __builtin_amdgcn_sched_barrier(0);
-        ds_finish(prv, pu, tf);
+        ds_finish(prv, wp, pu, tf);
         dp_prev = dp_cur;
       }
       __builtin_amdgcn_sched_barrier(0);
@@ -380,7 +395,7 @@ __global__ __launch_bounds__(256, 2) void lf_packed_dkv_kernel(PackedArgs a) {
       const int prv = (steps - 1) % 3;
       take_p(steps - 1, pu);
       first_half(buf[prv], tf);
-      ds_finish(prv, pu, tf);
+      ds_finish(prv, wi, pu, tf);
     }
   }
   if (!ok) return;
@@ -399,12 +414,11 @@ __global__ __launch_bounds__(256, 2) void lf_packed_dkv_kernel(PackedArgs a) {
 
 template <int D> int launch(const PackedArgs& a, hipStream_t st) {
   if (a.q_len > 0) {
-    const int64_t rows = (int64_t)a.H * a.q_len;
-    if (lf_launch(lf_packed_delta_kernel<D>, dim3((unsigned)((rows - 1) / (256 / (D / 8)) + 1)), dim3(256), 0, st, a) != hipSuccess) return LF_ERR_HIP;
-    const int64_t tiles = (int64_t)(a.q_len / 128 + a.seqs) * a.H;
     PackedArgs q = a;
     q.slots = a.q_len / 128 + a.seqs;
-    if (lf_launch(lf_packed_dq_kernel<D>, dim3((unsigned)tiles), dim3(256), 0, st, q) != hipSuccess) return LF_ERR_HIP;
+    const dim3 grid((unsigned)((int64_t)q.slots * a.H));
+    if (lf_launch(lf_packed_dq_kernel<D, true>, grid, dim3(256), 0, st, q) != hipSuccess) return LF_ERR_HIP;
+    if (lf_launch(lf_packed_dq_kernel<D, false>, grid, dim3(256), 0, st, q) != hipSuccess) return LF_ERR_HIP;
   }
   if (a.kv_len == 0) return LF_OK;
   return lf_launch(lf_packed_dkv_kernel<D>, dim3((unsigned)((int64_t)(a.kv_len / 64 + a.seqs) * a.Hk)), dim3(256), 0, st, a) == hipSuccess ? LF_OK : LF_ERR_HIP;
