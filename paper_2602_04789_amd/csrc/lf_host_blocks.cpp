@@ -235,7 +235,7 @@ extern "C" int lf_packed_attn(const void* Q, const void* K, const void* V, const
 
 extern "C" size_t lf_packed_attn_bwd_workspace_bytes(const lf_packed_shape* s) {
   if (!s || check_sizes(s) != LF_OK) return 0;
-  return (size_t)s->heads * s->q_len * sizeof(float);
+  return (size_t)s->heads * s->q_len * 2 * sizeof(float);
 }
 
 extern "C" int lf_packed_attn_bwd(const void* Q, const void* K, const void* V, const void* O, const void* dO, const float* lse2, const lf_packed_shape* s,

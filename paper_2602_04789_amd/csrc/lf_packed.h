@@ -12,7 +12,7 @@
 struct PackedArgs {
   const uint16_t *Q, *K, *V, *dO;
   uint16_t *O, *dQ, *dK, *dV;
-  float *lse2, *ndelta;
+  float *lse2, *ndelta, *nlse;   // nlse: -lse2 / c
   const int32_t *q_start, *kv_start;
   int64_t q_tok, q_head, k_tok, k_head, v_tok, v_head, o_tok, o_head;
   int H, Hk, G, seqs, q_len, kv_len, unit;
@@ -23,6 +23,7 @@ struct PackedArgs {
 };
 
 PackedArgs lf_packed_args(const lf_packed_call* c);
+int lf_launch_packed_dkv_wide(const PackedArgs& a, hipStream_t st);
 int lf_launch_packed_join(const PackedArgs& a, int d, int tile_rows, bool few, hipStream_t st);
 
 namespace {

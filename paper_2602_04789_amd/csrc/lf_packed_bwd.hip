@@ -162,7 +162,10 @@ __global__ __launch_bounds__(256, 2) void lf_packed_dq_kernel(PackedArgs a) {
       }
     }
     delta += __shfl_xor(delta, 32);
-    if (ok && kg == 0) a.ndelta[(int64_t)h * a.q_len + token] = -delta;
+    if (ok && kg == 0) {
+      a.ndelta[(int64_t)h * a.q_len + token] = -delta;
+      a.nlse[(int64_t)h * a.q_len + token] = -lse / a.c;
+    }
     return;
   }
   if (!ok) return;
@@ -421,6 +424,7 @@ template <int D> int launch(const PackedArgs& a, hipStream_t st) {
     if (lf_launch(lf_packed_dq_kernel<D, false>, grid, dim3(256), 0, st, q) != hipSuccess) return LF_ERR_HIP;
   }
   if (a.kv_len == 0) return LF_OK;
+  if (D == 128 && (int64_t)a.kv_len * a.Hk >= (int64_t)256 * 128) return lf_launch_packed_dkv_wide(a, st);
   return lf_launch(lf_packed_dkv_kernel<D>, dim3((unsigned)((int64_t)(a.kv_len / 64 + a.seqs) * a.Hk)), dim3(256), 0, st, a) == hipSuccess ? LF_OK : LF_ERR_HIP;
 }
 
@@ -429,6 +433,7 @@ template <int D> int launch(const PackedArgs& a, hipStream_t st) {
 int lf_launch_packed_bwd(const lf_packed_call* c, void* stream) {
   PackedArgs a = lf_packed_args(c);
   a.ndelta = (float*)c->workspace;
+  a.nlse = a.ndelta + (int64_t)a.H * a.q_len;
   a.parts = 1;
   return c->s->head_dim == 128 ? launch<128>(a, (hipStream_t)stream) : launch<64>(a, (hipStream_t)stream);
 }
