@@ -20,6 +20,7 @@ int lf_norm_fwd_rows(const lf_norm_shape* s, lf_norm_lay* lay);
 // Rows of a slot of the backward kernel, slots, and the floats of workspace: three sums a slot and channel, two a group and channel.
 struct lf_norm_slots {
   lf_norm_lay lay;
+  bool waves;          // a row for each of four wavefronts; `lay` is that of one
   int rows;
   int per_group;       // slots of a group (group_len > 0)
   int64_t slots, floats;

@@ -16,6 +16,8 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "lf_blocks.h"
 
 namespace {
@@ -40,11 +42,15 @@ struct NormArgs {
 template <int CTRL> __device__ __forceinline__ float turned(float v) {
   return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), CTRL, 0xf, 0xf, false));
 }
-__device__ __forceinline__ float wave_sum(float v) {
+__device__ __forceinline__ float row_sum16(float v) {
   v += turned<0x128>(v);      // row_ror:8, 4, 2, 1
   v += turned<0x124>(v);
   v += turned<0x122>(v);
   v += turned<0x121>(v);
+  return v;
+}
+__device__ __forceinline__ float wave_sum(float v) {
+  v = row_sum16(v);
   auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
   v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
   a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -69,10 +75,9 @@ struct RowSum {
     }
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      float s = p[i][0];
-      for (int w = 1; w < waves; ++w) s += p[i][w];
-      v[i] = s;
+    for (int i = 0; i < N; ++i) {         // a lane of 16 for each wavefront
+      const int w = threadIdx.x & 15;
+      v[i] = row_sum16(w < waves ? p[i][w] : 0.0f);
     }
   }
 };
@@ -163,9 +168,9 @@ __device__ __forceinline__ int group_start(const NormArgs& a, int g) {
   return min(max(a.starts[g], 0), a.L);
 }
 
-constexpr int most_threads(int nc) { return nc == 1 ? 640 : nc == 2 ? 1024 : 256; }
+constexpr int most_threads(int nc) { return nc == 2 ? 1024 : 256; }
 
-template <int NC, bool F32>
+template <int NC, bool F32, int AHEAD>
 __global__ __launch_bounds__(most_threads(NC)) void lf_gate_norm_kernel(NormArgs a) {
   __shared__ float place[2][2][kMaxWaves];
   RowSum row_sum = {place, (int)blockDim.x >> 6, (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6), 0};
@@ -195,16 +200,18 @@ __global__ __launch_bounds__(most_threads(NC)) void lf_gate_norm_kernel(NormArgs
     ch[i] = in[i] ? c : 0;
   }
   const bool has_b = a.B != nullptr, post = a.post != nullptr;
-  Raw<F32> xn[NC];
-  Raw<false> bn[NC];
-  auto request = [&](int row) __attribute__((always_inline)) {
+  Raw<F32> xn[AHEAD][NC];           // rows r, r + 1, ..
+  Raw<false> bn[AHEAD][NC];
+  auto request = [&](int row, int to) __attribute__((always_inline)) {
+    row = min(row, end - 1);
 #pragma unroll
     for (int i = 0; i < NC; ++i) {
-      xn[i] = load_raw<F32>(a.X, (int64_t)row * a.x_stride + ch[i]);
-      if (has_b) bn[i] = load_raw<false>(a.B, (int64_t)row * a.b_stride + ch[i]);
+      xn[to][i] = load_raw<F32>(a.X, (int64_t)row * a.x_stride + ch[i]);
+      if (has_b) bn[to][i] = load_raw<false>(a.B, (int64_t)row * a.b_stride + ch[i]);
     }
   };
-  request(r);
+#pragma unroll
+  for (int k = 0; k < AHEAD; ++k) request(r + k, k);
   float f[NC][8], sh[NC][8], ga[NC][8];
   int have = -1;
   const float count = (float)a.C;
@@ -216,8 +223,13 @@ __global__ __launch_bounds__(most_threads(NC)) void lf_gate_norm_kernel(NormArgs
     float x[NC][8], b[NC][8];
 #pragma unroll
     for (int i = 0; i < NC; ++i) {
-      unpack<F32>(xn[i], x[i]);
-      if (has_b) unpack<false>(bn[i], b[i]);
+      unpack<F32>(xn[0][i], x[i]);
+      if (has_b) unpack<false>(bn[0][i], b[i]);
+#pragma unroll
+      for (int k = 1; k < AHEAD; ++k) {
+        xn[k - 1][i] = xn[k][i];
+        if (has_b) bn[k - 1][i] = bn[k][i];
+      }
     }
     if (g != have) {
       have = g;
@@ -233,7 +245,7 @@ __global__ __launch_bounds__(most_threads(NC)) void lf_gate_norm_kernel(NormArgs
         }
       }
     }
-    if (r + 1 < end) request(r + 1);
+    if (r + AHEAD < end) request(r + AHEAD, AHEAD - 1);
     if (has_b) {
       if (post) {
         float ss[1] = {0.0f};
@@ -327,140 +339,232 @@ __device__ __forceinline__ Slot find_slot(const NormArgs& a, int64_t s) {
   return t;
 }
 
-template <int NC, bool F32>
-__global__ __launch_bounds__(most_threads(NC)) void lf_gate_norm_bwd_kernel(NormArgs a) {
+// How a workgroup of the backward kernel takes the rows of its slot.
+//   kRow      one at a time, the next two on their way
+//   kWaves    one for each of its four wavefronts (narrow rows: no barrier, and the four leave one set of sums)
+//   kWide     one at a time, for rows of more than 6 144 channels: values stay packed and are unpacked where they are used, tables are read from
+//             memory, and nothing is on its way, so that the sums fit the registers of 1 024 threads
+enum NormForm { kRow, kWaves, kWide };
+
+template <int NC, bool F32, int FORM, bool POST>
+__global__ __launch_bounds__(FORM == kWide ? 1024 : 256) void lf_gate_norm_bwd_kernel(NormArgs a) {
+  constexpr int AHEAD = FORM == kWide ? 1 : 2;
+  constexpr bool KEPT = FORM != kWide;
   __shared__ float place[2][2][kMaxWaves];
-  RowSum row_sum = {place, (int)blockDim.x >> 6, (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6), 0};
+  const int wave = (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  RowSum row_sum = {place, FORM == kWaves ? 1 : (int)blockDim.x >> 6, wave, 0};
   const Slot slot = find_slot(a, blockIdx.x);
   if (slot.r0 >= slot.r1) return;
+  const int step = FORM == kWaves ? 4 : 1, begin = slot.r0 + (FORM == kWaves ? wave : 0);
+  const int tid = FORM == kWaves ? threadIdx.x & 63 : threadIdx.x, across = FORM == kWaves ? 64 : blockDim.x;
   int ch[NC];
   bool in[NC];
 #pragma unroll
   for (int i = 0; i < NC; ++i) {
-    const int c = 8 * (int)(threadIdx.x + i * blockDim.x);
+    const int c = 8 * (tid + i * across);
     in[i] = c < a.C;
     ch[i] = in[i] ? c : 0;
   }
-  const bool has_b = a.B != nullptr, post = a.post != nullptr;
+  const bool has_b = a.B != nullptr;
   const float count = (float)a.C;
-  Raw<F32> xn[NC], on[NC];
-  Raw<false> bn[NC], yn[NC];
-  auto request = [&](int row) __attribute__((always_inline)) {
+  // What a thread without channels in a chunk holds is zeros: its dY, D and B add nothing.
+  Raw<F32> xn[AHEAD][NC] = {}, on[AHEAD][NC] = {};
+  Raw<false> bn[AHEAD][NC] = {}, yn[AHEAD][NC] = {};
+  auto request = [&](int row, int to) __attribute__((always_inline)) {
+    row = min(row, slot.r1 - 1);
 #pragma unroll
-    for (int i = 0; i < NC; ++i) {
-      xn[i] = load_raw<F32>(a.Xout, (int64_t)row * a.xo_stride + ch[i]);
-      if (a.dXout) on[i] = load_raw<F32>(a.dXout, (int64_t)row * a.xo_stride + ch[i]);
-      if (a.dY) yn[i] = load_raw<false>(a.dY, (int64_t)row * a.y_stride + ch[i]);
-      if (has_b) bn[i] = load_raw<false>(a.B, (int64_t)row * a.b_stride + ch[i]);
-    }
+    for (int i = 0; i < NC; ++i)
+      if (in[i]) {
+        xn[to][i] = load_raw<F32>(a.Xout, (int64_t)row * a.xo_stride + ch[i]);
+        if (a.dXout) on[to][i] = load_raw<F32>(a.dXout, (int64_t)row * a.xo_stride + ch[i]);
+        if (a.dY) yn[to][i] = load_raw<false>(a.dY, (int64_t)row * a.y_stride + ch[i]);
+        if (has_b) bn[to][i] = load_raw<false>(a.B, (int64_t)row * a.b_stride + ch[i]);
+      }
   };
-  request(slot.r0);
+  if constexpr (FORM != kWide) {
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) request(begin + k * step, k);
+  }
   float S[NC][8], Z[NC][8], T[NC][8];
 #pragma unroll
   for (int i = 0; i < NC; ++i)
 #pragma unroll
     for (int e = 0; e < 8; ++e) S[i][e] = Z[i][e] = T[i][e] = 0.0f;
-  for (int r = slot.r0; r < slot.r1; ++r) {
-    float n[NC][8], dy[NC][8], D[NC][8], b[NC][8];
+  // the group's factors: of Y, and of B
+  auto factors_y = [&](int i, float (&f)[8]) __attribute__((always_inline)) { load_factor(a, slot.g, ch[i], f); };
+  auto factors_b = [&](int i, float (&ga)[8]) __attribute__((always_inline)) {
+    if (a.gate) load_table(a.gate + (int64_t)slot.g * a.gate_stride + ch[i], ga);
+    float w[8];
+    if constexpr (POST) load_table(a.post + ch[i], w);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      ga[e] = a.gate ? ga[e] * a.rs : a.rs;
+      if constexpr (POST) ga[e] *= w[e];
+    }
+  };
+  constexpr int KN = KEPT ? NC : 1;         // what is kept over the slot, or over a row: chunks
+  float f[KN][8], ga[KN][8];
+  if constexpr (KEPT) {
 #pragma unroll
     for (int i = 0; i < NC; ++i) {
-      unpack<F32>(xn[i], n[i]);
-      if (a.dXout) unpack<F32>(on[i], D[i]);
-      if (a.dY) unpack<false>(yn[i], dy[i]);
-      if (has_b) unpack<false>(bn[i], b[i]);
+      factors_y(i, f[i]);
+      factors_b(i, ga[i]);
+    }
+  }
+  for (int r = begin; r < slot.r1; r += step) {
+    Raw<F32> xr[NC], orw[NC];
+    Raw<false> br[NC], yr[NC];
+    if constexpr (FORM == kWide) request(r, 0);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        if (!a.dXout) D[i][e] = 0.0f;
-        if (!a.dY) dy[i][e] = 0.0f;
-        if (!in[i]) n[i][e] = dy[i][e] = D[i][e] = b[i][e] = 0.0f;
+    for (int i = 0; i < NC; ++i) {
+      xr[i] = xn[0][i];
+      orw[i] = on[0][i];
+      br[i] = bn[0][i];
+      yr[i] = yn[0][i];
+#pragma unroll
+      for (int k = 1; k < AHEAD; ++k) {
+        xn[k - 1][i] = xn[k][i];
+        on[k - 1][i] = on[k][i];
+        bn[k - 1][i] = bn[k][i];
+        yn[k - 1][i] = yn[k][i];
       }
     }
-    if (r + 1 < slot.r1) request(r + 1);
-    // the row's mean, and its squares (of B too)
+    float n[KN][8], u[KN][8];
+    // the row's mean, and the squares of B
     float first[2] = {0.0f, 0.0f};
 #pragma unroll
     for (int i = 0; i < NC; ++i) {
-      float s = 0.0f, q = 0.0f;
+      float (&m)[8] = n[KEPT ? i : 0];
+      unpack<F32>(xr[i], m);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        s += n[i][e];
-        if (post) q = fmaf(b[i][e], b[i][e], q);
+      for (int e = 0; e < 8; ++e) first[0] += m[e];
+      if constexpr (POST) {
+        float b[8];
+        unpack<false>(br[i], b);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) first[1] = fmaf(b[e], b[e], first[1]);
       }
-      first[0] += s;
-      first[1] += q;
     }
-    if (a.layer || post) row_sum(first);
+    if constexpr (FORM != kWide) {
+      if (r + AHEAD * step < slot.r1) request(r + AHEAD * step, AHEAD - 1);
+    }
+    if (a.layer || POST) row_sum(first);
     const float mean = a.layer ? first[0] / count : 0.0f;
-    const float rb = post ? 1.0f / sqrtf(first[1] / count + a.eps) : 1.0f;
+    const float rb = POST ? 1.0f / sqrtf(first[1] / count + a.eps) : 1.0f;
     float ss[1] = {0.0f};
 #pragma unroll
     for (int i = 0; i < NC; ++i) {
+      float (&m)[8] = n[KEPT ? i : 0];
+      if constexpr (!KEPT) unpack<F32>(xr[i], m);
       float s = 0.0f;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        n[i][e] -= mean;
-        s = fmaf(n[i][e], n[i][e], s);
+        m[e] -= mean;
+        s = fmaf(m[e], m[e], s);
       }
       ss[0] += in[i] ? s : 0.0f;
     }
     row_sum(ss);
     const float inv = 1.0f / sqrtf(ss[0] / count + a.eps);
-    float means[2] = {0.0f, 0.0f};
-    float f[NC][8];
-#pragma unroll
-    for (int i = 0; i < NC; ++i) {
-      load_factor(a, slot.g, ch[i], f[i]);
-      float s = 0.0f, q = 0.0f;
+    // n and dY f of a chunk
+    auto values = [&](int i, bool first_time) __attribute__((always_inline)) {
+      float (&m)[8] = n[KEPT ? i : 0];
+      float (&w)[8] = u[KEPT ? i : 0];
+      if constexpr (!KEPT) {
+        unpack<F32>(xr[i], m);
+        factors_y(i, f[0]);
+      } else if (!first_time) {
+        return;
+      }
+      float dy[8];
+      unpack<false>(yr[i], dy);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        n[i][e] = in[i] ? n[i][e] * inv : 0.0f;
-        S[i][e] = fmaf(dy[i][e], n[i][e], S[i][e]);
-        Z[i][e] += dy[i][e];
-        dy[i][e] *= f[i][e];
-        s += dy[i][e];
-        q = fmaf(dy[i][e], n[i][e], q);
+        m[e] = KEPT ? m[e] * inv : (m[e] - mean) * inv;
+        w[e] = dy[e] * f[KEPT ? i : 0][e];
+        if (first_time) {
+          S[i][e] = fmaf(dy[e], m[e], S[i][e]);
+          Z[i][e] += dy[e];
+        }
       }
-      means[0] += s;
-      means[1] += q;
+    };
+    float means[2] = {0.0f, 0.0f};
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+      values(i, true);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        means[0] += u[KEPT ? i : 0][e];
+        means[1] = fmaf(u[KEPT ? i : 0][e], n[KEPT ? i : 0][e], means[1]);
+      }
     }
     row_sum(means);
     const float mu = a.layer ? means[0] / count : 0.0f, mun = means[1] / count;
     float eb[1] = {0.0f};
+    float E[NC][8];              // what goes on to B
 #pragma unroll
     for (int i = 0; i < NC; ++i) {
+      values(i, false);
+      float D[8], b[8];
+      unpack<F32>(orw[i], D);
+      unpack<false>(br[i], b);
+      if constexpr (!KEPT) {
+        if (has_b) factors_b(i, ga[0]);
+      }
 #pragma unroll
-      for (int e = 0; e < 8; ++e) D[i][e] = fmaf(inv, fmaf(-n[i][e], mun, dy[i][e] - mu), D[i][e]);
-      if (in[i]) store_raw<F32>(a.dX, (int64_t)r * a.xo_stride + ch[i], pack<F32>(D[i]));
-      if (has_b) {
-        float ga[8], w[8];
-        if (a.gate) load_table(a.gate + (int64_t)slot.g * a.gate_stride + ch[i], ga);
-        if (post) load_table(a.post + ch[i], w);
-        float s = 0.0f;
+      for (int e = 0; e < 8; ++e) D[e] = fmaf(inv, fmaf(-n[KEPT ? i : 0][e], mun, u[KEPT ? i : 0][e] - mu), D[e]);
+      if (in[i]) store_raw<F32>(a.dX, (int64_t)r * a.xo_stride + ch[i], pack<F32>(D));
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          D[i][e] *= a.rs;
-          b[i][e] *= rb;
-          T[i][e] = fmaf(b[i][e], D[i][e], T[i][e]);
-          if (a.gate) D[i][e] *= ga[e];
-          if (post) D[i][e] *= w[e];
-          s = fmaf(D[i][e], b[i][e], s);
-        }
-        eb[0] += in[i] ? s : 0.0f;
+      for (int e = 0; e < 8; ++e) {
+        if constexpr (POST) b[e] *= rb;
+        T[i][e] = fmaf(b[e], D[e], T[i][e]);
+        E[i][e] = D[e] * ga[KEPT ? i : 0][e];
+        if constexpr (POST) eb[0] = fmaf(E[i][e], b[e], eb[0]);      // (zero without channels: b is)
       }
     }
     if (has_b) {
-      if (post) row_sum(eb);
-      const float m = post ? eb[0] / count : 0.0f;
+      if constexpr (POST) {
+        row_sum(eb);
+        const float m = eb[0] / count;
 #pragma unroll
-      for (int i = 0; i < NC; ++i) {
+        for (int i = 0; i < NC; ++i) {
+          float b[8];
+          unpack<false>(br[i], b);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) D[i][e] = rb * fmaf(-b[i][e], m, D[i][e]);
-        if (in[i]) store_raw<false>(a.dB, (int64_t)r * a.b_stride + ch[i], pack<false>(D[i]));
+          for (int e = 0; e < 8; ++e) E[i][e] = rb * fmaf(-b[e] * rb, m, E[i][e]);
+        }
       }
+#pragma unroll
+      for (int i = 0; i < NC; ++i)
+        if (in[i]) store_raw<false>(a.dB, (int64_t)r * a.b_stride + ch[i], pack<false>(E[i]));
     }
   }
   if (!a.part) return;
   float* p = a.part + (int64_t)blockIdx.x * 3 * a.C;
+  if constexpr (FORM == kWaves) {       // the four wavefronts' sums become one, in their order
+    __shared__ float both[3][NC * 8][64];
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+      if (wave > 0) {
+#pragma unroll
+        for (int i = 0; i < NC; ++i)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) both[wave - 1][8 * i + e][tid] = k == 0 ? S[i][e] : k == 1 ? Z[i][e] : T[i][e];
+      }
+      __syncthreads();
+      if (wave == 0) {
+#pragma unroll
+        for (int i = 0; i < NC; ++i)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            float& v = k == 0 ? S[i][e] : k == 1 ? Z[i][e] : T[i][e];
+            v = v + both[0][8 * i + e][tid] + both[1][8 * i + e][tid] + both[2][8 * i + e][tid];
+          }
+      }
+      __syncthreads();
+    }
+    if (wave > 0) return;
+  }
 #pragma unroll
   for (int i = 0; i < NC; ++i)
     if (in[i]) {
@@ -484,11 +588,13 @@ struct SumArgs {
   float *dgate, *dscale, *dshift;
   float* sums;           // [groups][2][C]: S and T, for the weights; or null
 };
-// A group's slots: 16 channels of a workgroup, its 16 rows of threads taking every 16th slot and joined in their order.
-__global__ __launch_bounds__(256) void lf_gate_norm_sum_kernel(SumArgs b) {
+// A group's slots: 16 channels of a workgroup, its rows of threads (16, or 64 for groups of many slots) taking a slot in turn, four of them at a time, and joined
+// in their order.
+template <int kSumRows>
+__global__ __launch_bounds__(16 * kSumRows) void lf_gate_norm_sum_kernel(SumArgs b) {
   const NormArgs& a = b.n;
-  __shared__ float s[3][16][17];
-  const int c = blockIdx.x * 16 + (threadIdx.x & 15), lane = threadIdx.x >> 4;
+  __shared__ float s[3][kSumRows][17];
+  const int col = threadIdx.x & 15, c = blockIdx.x * 16 + col, row = threadIdx.x >> 4;
   for (int g = blockIdx.y; g < a.groups; g += gridDim.y) {
     int64_t first, many;
     if (a.group_len > 0) {
@@ -502,31 +608,39 @@ __global__ __launch_bounds__(256) void lf_gate_norm_sum_kernel(SumArgs b) {
     }
     float v[3] = {0.0f, 0.0f, 0.0f};
     if (c < a.C) {
-      for (int64_t i = lane; i < many; i += 16) {
-        const float* p = a.part + (first + i) * 3 * a.C + c;
+      const float* p = a.part + first * 3 * a.C + c;
+      for (int64_t i = row; i < many; i += 4 * kSumRows) {
+        float y[4][3];
 #pragma unroll
-        for (int k = 0; k < 3; ++k) v[k] += p[(int64_t)k * a.C];
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+          for (int k = 0; k < 3; ++k) y[u][k] = i + u * kSumRows < many ? p[((i + u * kSumRows) * 3 + k) * a.C] : 0.0f;
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+          for (int k = 0; k < 3; ++k) v[k] += y[u][k];
       }
     }
     __syncthreads();
 #pragma unroll
-    for (int k = 0; k < 3; ++k) s[k][lane][threadIdx.x & 15] = v[k];
+    for (int k = 0; k < 3; ++k) s[k][row][col] = v[k];
     __syncthreads();
-    if (lane == 0 && c < a.C) {
+    if (row < 3) {              // a sum each: three rows of threads
+      float t = 0.0f;
 #pragma unroll
-      for (int k = 0; k < 3; ++k) {
-        float t = 0.0f;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) t += s[k][i][threadIdx.x & 15];
-        v[k] = t;
-      }
+      for (int i = 0; i < kSumRows; ++i) t += s[row][i][col];
       const int64_t at = (int64_t)g * a.C + c;
-      if (b.dscale) b.dscale[at] = a.weight ? v[0] * a.weight[c] : v[0];
-      if (b.dshift) b.dshift[at] = v[1];
-      if (b.dgate) b.dgate[at] = a.post ? v[2] * a.post[c] : v[2];
-      if (b.sums) {
-        b.sums[2 * (int64_t)g * a.C + c] = v[0];
-        b.sums[(2 * (int64_t)g + 1) * a.C + c] = v[2];
+      if (c < a.C) {
+        if (row == 0) {
+          if (b.dscale) b.dscale[at] = a.weight ? t * a.weight[c] : t;
+          if (b.sums) b.sums[2 * (int64_t)g * a.C + c] = t;
+        } else if (row == 1) {
+          if (b.dshift) b.dshift[at] = t;
+        } else {
+          t *= a.rs;
+          if (b.dgate) b.dgate[at] = a.post ? t * a.post[c] : t;
+          if (b.sums) b.sums[(2 * (int64_t)g + 1) * a.C + c] = t;
+        }
       }
     }
   }
@@ -582,9 +696,9 @@ int lf_launch_gate_norm(const lf_norm_call* c, void* stream) {
   lf_norm_lay l;
   a.rows = lf_norm_fwd_rows(c->s, &l);
   const bool f32 = c->s->stream_dtype == LF_F32;
-  auto kernel = l.nc == 1 ? (f32 ? lf_gate_norm_kernel<1, true> : lf_gate_norm_kernel<1, false>)
-              : l.nc == 2 ? (f32 ? lf_gate_norm_kernel<2, true> : lf_gate_norm_kernel<2, false>)
-                          : (f32 ? lf_gate_norm_kernel<3, true> : lf_gate_norm_kernel<3, false>);
+  auto kernel = l.nc == 1 ? (f32 ? lf_gate_norm_kernel<1, true, 1> : lf_gate_norm_kernel<1, false, 1>)
+              : l.nc == 2 ? (f32 ? lf_gate_norm_kernel<2, true, 1> : lf_gate_norm_kernel<2, false, 1>)
+                          : (f32 ? lf_gate_norm_kernel<3, true, 2> : lf_gate_norm_kernel<3, false, 2>);
   const unsigned blocks = (unsigned)((a.L - 1) / a.rows + 1);
   return lf_launch(kernel, dim3(blocks), dim3(l.threads), 0, (hipStream_t)stream, a) == hipSuccess ? LF_OK : LF_ERR_HIP;
 }
@@ -597,16 +711,25 @@ int lf_launch_gate_norm_bwd(const lf_norm_call* c, void* stream) {
   const bool sums = c->dgate || c->dpost_weight || c->dweight || c->dscale || c->dshift;
   a.part = sums ? c->workspace : nullptr;
   const bool f32 = c->s->stream_dtype == LF_F32;
-  auto kernel = n.lay.nc == 1 ? (f32 ? lf_gate_norm_bwd_kernel<1, true> : lf_gate_norm_bwd_kernel<1, false>)
-              : n.lay.nc == 2 ? (f32 ? lf_gate_norm_bwd_kernel<2, true> : lf_gate_norm_bwd_kernel<2, false>)
-                              : (f32 ? lf_gate_norm_bwd_kernel<3, true> : lf_gate_norm_bwd_kernel<3, false>);
+  auto pick = [&](auto post) {
+    constexpr bool P = decltype(post)::value;
+    if (n.waves)
+      return n.lay.nc == 1 ? (f32 ? lf_gate_norm_bwd_kernel<1, true, kWaves, P> : lf_gate_norm_bwd_kernel<1, false, kWaves, P>)
+           : n.lay.nc == 2 ? (f32 ? lf_gate_norm_bwd_kernel<2, true, kWaves, P> : lf_gate_norm_bwd_kernel<2, false, kWaves, P>)
+                           : (f32 ? lf_gate_norm_bwd_kernel<3, true, kWaves, P> : lf_gate_norm_bwd_kernel<3, false, kWaves, P>);
+    return n.lay.nc == 3 ? (f32 ? lf_gate_norm_bwd_kernel<3, true, kRow, P> : lf_gate_norm_bwd_kernel<3, false, kRow, P>)
+                         : (f32 ? lf_gate_norm_bwd_kernel<2, true, kWide, P> : lf_gate_norm_bwd_kernel<2, false, kWide, P>);
+  };
+  auto kernel = c->post_weight ? pick(std::true_type{}) : pick(std::false_type{});
   hipStream_t st = (hipStream_t)stream;
-  if (lf_launch(kernel, dim3((unsigned)n.slots), dim3(n.lay.threads), 0, st, a) != hipSuccess) return LF_ERR_HIP;
+  if (lf_launch(kernel, dim3((unsigned)n.slots), dim3(n.waves ? 256 : n.lay.threads), 0, st, a) != hipSuccess) return LF_ERR_HIP;
   if (!sums) return LF_OK;
   const bool weights = c->dweight || c->dpost_weight;
   SumArgs b = {a, c->dgate, c->dscale, c->dshift, weights ? c->workspace + n.slots * 3 * a.C : nullptr};
   const unsigned across = (unsigned)(a.C + 15) / 16;
-  if (lf_launch(lf_gate_norm_sum_kernel, dim3(across, (unsigned)(a.groups < 8192 ? a.groups : 8192)), dim3(256), 0, st, b) != hipSuccess)
+  const dim3 grid(across, (unsigned)(a.groups < 4096 ? a.groups : 4096));
+  const bool many = n.slots > 64 * (int64_t)a.groups;
+  if ((many ? lf_launch(lf_gate_norm_sum_kernel<64>, grid, dim3(1024), 0, st, b) : lf_launch(lf_gate_norm_sum_kernel<16>, grid, dim3(256), 0, st, b)) != hipSuccess)
     return LF_ERR_HIP;
   if (!weights) return LF_OK;
   return lf_launch(lf_gate_norm_weight_kernel, dim3(across), dim3(256), 0, st, b, c->dweight, c->dpost_weight) == hipSuccess ? LF_OK : LF_ERR_HIP;

@@ -39,7 +39,7 @@ int first_error(const int* rc, int n) {
 }
 int check_slots(const lf_norm_shape* s) {
   const lf_norm_slots n = lf_norm_bwd_slots(s);
-  return n.slots * n.lay.threads < kMostThreads && n.floats <= (int64_t)1 << 38 ? LF_OK : LF_ERR_SHAPE;
+  return n.slots * (n.waves ? 256 : n.lay.threads) < kMostThreads && n.floats <= (int64_t)1 << 38 ? LF_OK : LF_ERR_SHAPE;
 }
 
 // ---- packed attention ----
@@ -93,22 +93,31 @@ float scale_or_default(float s, int d) { return s > 0.0f ? s : 1.0f / sqrtf((flo
 }  // namespace
 
 int lf_norm_fwd_rows(const lf_norm_shape* s, lf_norm_lay* lay) {
-  *lay = lf_lay_norm(s->channels, s->channels <= 640 * 8 ? 1 : 2);
-  const int64_t blocks = 256 * 32 / (lay->threads / 64);
+  const int chunks = s->channels / 8;
+  *lay = lf_lay_norm(s->channels, chunks <= 256 ? 1 : chunks <= 768 ? 3 : 2);
+  const int64_t blocks = 256 * 64 / (lay->threads / 64);
   return (int)((s->tokens - 1) / blocks + 1);
 }
 
 lf_norm_slots lf_norm_bwd_slots(const lf_norm_shape* s) {
+  const int chunks = s->channels / 8;
   lf_norm_slots n;
-  n.lay = lf_lay_norm(s->channels, s->channels <= 640 * 8 ? 1 : 2);
-  const int64_t blocks = 256 * 12 / (n.lay.threads / 64) + 1;
-  n.rows = (int)((s->tokens - 1) / blocks + 1);
+  n.waves = chunks <= 192;
+  n.lay = lf_lay_norm(s->channels, n.waves ? (chunks + 63) / 64 : chunks <= 768 ? 3 : 2);
+  // as many slots as the chip has room for at once: with two or three chunks to a thread a SIMD holds one wavefront, with one three of them
+  const int waves = n.lay.threads / 64;
+  const int64_t at_once = 256 * (n.waves ? (n.lay.nc == 1 ? 3 : 1) : n.lay.nc == 3 ? 4 / waves : 1);
   if (s->group_len > 0) {
+    const int64_t each = at_once / s->groups > 1 ? at_once / s->groups : 1;      // slots of a group
+    n.rows = (int)((s->group_len - 1) / each + 1);
+    if (n.waves && n.rows < 4) n.rows = 4;
     if (n.rows > s->group_len) n.rows = s->group_len;
     n.per_group = (s->group_len - 1) / n.rows + 1;
     n.slots = (int64_t)n.per_group * s->groups;
   } else {
     n.per_group = 0;
+    n.rows = (int)((s->tokens - 1) / (at_once > 2 * s->groups ? at_once - s->groups : at_once / 2) + 1);
+    if (n.waves && n.rows < 4) n.rows = 4;
     n.slots = (int64_t)s->tokens / n.rows + s->groups;
   }
   n.floats = (n.slots * 3 + (int64_t)s->groups * 2) * s->channels;
@@ -193,8 +202,10 @@ lf_packed_plan lf_plan_packed(const lf_packed_shape* s) {
   int64_t each = want > 1 ? (mean * tiles / want + 63) / 64 * 64 : (int64_t)1 << 30;
   if (each < 512) each = 512;
   if (each > 1 << 30) each = 1 << 30;
-  int64_t parts = (s->kv_len + each - 1) / each;
-  if (s->kv_len <= 1024) parts = 1;
+  // the longest sequence is taken to be four times the mean one
+  const int64_t longest = s->kv_len < 4 * mean ? s->kv_len : 4 * mean;
+  int64_t parts = (longest + each - 1) / each;
+  if (longest <= 1024) parts = 1;
   if (parts < 1) parts = 1;
   if (parts > LF_PACKED_MAX_PARTS) parts = LF_PACKED_MAX_PARTS;
   p.parts = (int)parts;

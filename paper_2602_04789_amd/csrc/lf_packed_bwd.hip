@@ -1,7 +1,7 @@
 // Backward pass of the packed attention.  With P = exp2(s c - lse2), delta_x = dO_x . O_x, dP = dO V^T, dS = P (dP - delta):
 //   dV_y = sum_x P dO_x      dQ_x = scale sum_y dS k_y      dK_y = scale sum_x dS q_x     (dK and dV over the heads that share the head, too)
 //
-// No atomics, every launch owns its outputs: one leaves -delta, one owns rows and walks the tokens they see (dQ), one owns tokens and walks the
+// No atomics, every launch owns its outputs: one owns rows and walks the tokens they see (dQ; it leaves delta for the other), one owns tokens and walks the
 // rows that see them, head by head (dK, dV).  Both recompute the scores.  As in the forward kernel the score-like products take their A operand from tiles in
 // LDS and their B operand from the owner's rows in registers; P and dS are then the B operand of the accumulating products, whose A operand
 // is the same tile through the transposing read.  Matrix work bounds both: seven products for the five that the mathematics counts.
@@ -23,8 +23,8 @@ template <int CH> constexpr int kTrHiFlip = CH == 16 ? 16 : 0;
 // sequences of one to four tokens: dQ off by 4.8e-3 in the 2-norm).
 constexpr int kShort = 256;
 
-// dQ: four wavefronts of 32 rows each share tiles of 32 tokens of K and V.  DELTA: the launch before it, -delta of every row.
-template <int D, bool DELTA>
+// dQ, and -delta and -lse2 / c of every row for the launch behind it: four wavefronts of 32 rows each share tiles of 32 tokens of K and V.
+template <int D>
 __global__ __launch_bounds__(256, 2) void lf_packed_dq_kernel(PackedArgs a) {
   constexpr int kRows = 128;
   constexpr int CH = D / 8, KS = D / 16, MB = D / 32;
@@ -54,7 +54,7 @@ __global__ __launch_bounds__(256, 2) void lf_packed_dq_kernel(PackedArgs a) {
   const bool active = 32 * wave < rows;
   const int lim_first = s.nk == 1 || row_limit(s, a.unit, i0 + 32 * wave) <= 1 ? 0 : row_limit(s, a.unit, i0 + 32 * wave);
   const int lim_last = active ? row_limit(s, a.unit, i0 + min(32 * wave + 31, rows - 1)) : 0;
-  const int seen_all = row_limit(s, a.unit, i0 + rows - 1), seen = DELTA && seen_all > kShort ? 0 : seen_all;
+  const int seen = row_limit(s, a.unit, i0 + rows - 1);
 
   Frag qf[KS], gf[KS];
 #pragma unroll
@@ -65,10 +65,9 @@ __global__ __launch_bounds__(256, 2) void lf_packed_dq_kernel(PackedArgs a) {
       gf[k].u = *reinterpret_cast<const u32x4*>(a.dO + (int64_t)h * a.o_head + token * a.o_tok + 16 * k + 8 * kg);
     }
   }
-  float lse = INFINITY, nd = 0.0f, delta = 0.0f;
+  float lse = INFINITY, delta = 0.0f;
   if (ok) {
     lse = a.lse2[(int64_t)h * a.q_len + token];
-    if constexpr (!DELTA) nd = a.ndelta[(int64_t)h * a.q_len + token];
   }
   const uint16_t* Kh = a.K + (int64_t)hk * a.k_head;
   const uint16_t* Vh = a.V + (int64_t)hk * a.v_head;
@@ -99,20 +98,16 @@ __global__ __launch_bounds__(256, 2) void lf_packed_dq_kernel(PackedArgs a) {
       tbase[mb] = (tr_row * CH + both_swz<CH>(tr_row, col >> 3)) * 8 + (col & 7);
     }
   }
-  f32x16 acc[MB], nd16;
-#pragma unroll
-  for (int mb = 0; mb < MB; ++mb) acc[mb] = zero16();
-#pragma unroll
-  for (int i = 0; i < 16; ++i) nd16[i] = nd;
-
-  auto work = [&](int t, const u32x4* at) __attribute__((always_inline)) {
+  f32x16 nd16 = zero16();
+  auto scores = [&](int t, const u32x4* at, f32x16& sc, f32x16& dp) __attribute__((always_inline)) {
     Frag kf[KS], vf[KS];
 #pragma unroll
     for (int k = 0; k < KS; ++k) {
       kf[k].u = at[kaddr[k]];
       vf[k].u = at[T32 + vaddr[k]];
     }
-    f32x16 sc = zero16(), dp = nd16;
+    sc = zero16();
+    dp = nd16;
 #pragma unroll
     for (int k = 0; k < KS; ++k) {
       sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[k].v, qf[k].v, sc, 0, 0, 0);
@@ -123,11 +118,50 @@ __global__ __launch_bounds__(256, 2) void lf_packed_dq_kernel(PackedArgs a) {
       for (int i = 0; i < 16; ++i)
         if (t + 8 * (i >> 2) + 4 * kg + (i & 3) >= lim) sc[i] = -INFINITY;
     }
-    if constexpr (DELTA) {
+  };
+  // every tile of tokens that the workgroup's rows see, in turn
+  auto walk = [&](auto work) __attribute__((always_inline)) {
+    if (seen > 0) request(0, stage[0]);
+    int cur = 0;
+    for (int t = 0; t < seen; t += kTile, cur ^= 1) {
+      __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+      lds_barrier();
+      if (t + kTile < seen) request(t + kTile, stage[cur ^ 1]);
+      if (t < lim_last) work(t, stage[cur]);
+    }
+  };
+  if (seen <= kShort) {
+    walk([&](int t, const u32x4* at) __attribute__((always_inline)) {
+      f32x16 sc, dp;
+      scores(t, at, sc, dp);
 #pragma unroll
       for (int i = 0; i < 16; ++i) delta = fmaf(__builtin_amdgcn_exp2f(fmaf(sc[i], a.c, -lse)), dp[i], delta);
-      return;
+    });
+    lds_barrier();                  // the second walk begins in the first stage
+  } else if (ok) {
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+      const u32x4 o = *reinterpret_cast<const u32x4*>(a.O + (int64_t)h * a.o_head + token * a.o_tok + 16 * k + 8 * kg);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        delta = fmaf(__uint_as_float(o[e] << 16), __uint_as_float(gf[k].u[e] << 16), delta);
+        delta = fmaf(__uint_as_float(o[e] & 0xffff0000u), __uint_as_float(gf[k].u[e] & 0xffff0000u), delta);
+      }
     }
+  }
+  delta += __shfl_xor(delta, 32);
+  if (ok && kg == 0) {
+    a.ndelta[(int64_t)h * a.q_len + token] = -delta;
+    a.nlse[(int64_t)h * a.q_len + token] = -lse / a.c;
+  }
+#pragma unroll
+  for (int i = 0; i < 16; ++i) nd16[i] = -delta;
+  f32x16 acc[MB];
+#pragma unroll
+  for (int mb = 0; mb < MB; ++mb) acc[mb] = zero16();
+  walk([&](int t, const u32x4* at) __attribute__((always_inline)) {
+    f32x16 sc, dp;
+    scores(t, at, sc, dp);
     bf16x8 ds[2];
 #pragma unroll
     for (int i = 0; i < 16; ++i) ds[i >> 3][i & 7] = (__bf16)(__builtin_amdgcn_exp2f(fmaf(sc[i], a.c, -lse)) * dp[i]);
@@ -140,34 +174,7 @@ __global__ __launch_bounds__(256, 2) void lf_packed_dq_kernel(PackedArgs a) {
         const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(LDS_PTR(bf16x4, k16 + (tbase[mb] ^ kTrHiFlip<CH>) + (16 * u + 8) * CH * 8));
         acc[mb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7), ds[u], acc[mb], 0, 0, 0);
       }
-  };
-  if (seen > 0) request(0, stage[0]);
-  int cur = 0;
-  for (int t = 0; t < seen; t += kTile, cur ^= 1) {
-    __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
-    lds_barrier();
-    if (t + kTile < seen) request(t + kTile, stage[cur ^ 1]);
-    if (t < lim_last) work(t, stage[cur]);
-  }
-  if constexpr (DELTA) {
-    if (seen_all > kShort && ok) {
-#pragma unroll
-      for (int k = 0; k < KS; ++k) {
-        const u32x4 o = *reinterpret_cast<const u32x4*>(a.O + (int64_t)h * a.o_head + token * a.o_tok + 16 * k + 8 * kg);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          delta = fmaf(__uint_as_float(o[e] << 16), __uint_as_float(gf[k].u[e] << 16), delta);
-          delta = fmaf(__uint_as_float(o[e] & 0xffff0000u), __uint_as_float(gf[k].u[e] & 0xffff0000u), delta);
-        }
-      }
-    }
-    delta += __shfl_xor(delta, 32);
-    if (ok && kg == 0) {
-      a.ndelta[(int64_t)h * a.q_len + token] = -delta;
-      a.nlse[(int64_t)h * a.q_len + token] = -lse / a.c;
-    }
-    return;
-  }
+  });
   if (!ok) return;
   uint16_t* op = a.dQ + (int64_t)h * a.q_head + token * a.q_tok;
 #pragma unroll
@@ -183,17 +190,22 @@ __global__ __launch_bounds__(256, 2) void lf_packed_dq_kernel(PackedArgs a) {
 
 // dK and dV of 64 tokens: wavefront (rh, role) has 32 of them.  Role 0 computes S = Q K^T, P and dV^T += dO^T P, role 1 dP = dO V^T, dS and
 // dK^T += Q^T dS a step later, with the P that its partner has left in LDS; so a tile of rows lives for two steps (three stages), and one barrier a step
-// is enough.
-template <int D>
-__global__ __launch_bounds__(256, 2) void lf_packed_dkv_kernel(PackedArgs a) {
+// is enough.  SPLIT > 1: the workgroup holds SPLIT such groups with stages of their own, each takes a share of the steps (all the same number; those past
+// the end are empty), and their sums are added through LDS in order: for calls with too few tokens to fill the chip.
+template <int D, int SPLIT>
+__global__ __launch_bounds__(256 * SPLIT, SPLIT == 1 ? 2 : 1) void lf_packed_dkv_kernel(PackedArgs a) {
   constexpr int kTokens = 64;
   constexpr int CH = D / 8, KS = D / 16, MB = D / 32;
   constexpr int T32 = kTile * CH;
   constexpr int LPW = T32 / 64 / 4;
   constexpr int RPI = 64 / CH;
-  __shared__ u32x4 buf[3][2 * T32];          // [step mod 3][Q | dO]
-  __shared__ f32x4 st[3][4][16];             // lse2 (role 0) or -delta of the 32 rows, for each wavefront; the upper half takes what the other lanes load
-  __shared__ u32x4 ph[2][2][2][64];          // P: [step parity][rh][k-step][lane]
+  __shared__ u32x4 buf_all[SPLIT][3][2 * T32];   // [step mod 3][Q | dO]
+  __shared__ f32x4 st_all[SPLIT][3][4][16];      // lse2 (role 0) or -delta of the 32 rows, for each wavefront; the upper half takes what the other lanes load
+  __shared__ u32x4 ph_all[SPLIT][2][2][2][64];   // P: [step parity][rh][k-step][lane]
+  const int group = SPLIT > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 8) : 0;
+  u32x4 (*const buf)[2 * T32] = buf_all[group];
+  f32x4 (*const st)[4][16] = st_all[group];
+  u32x4 (*const ph)[2][2][64] = ph_all[group];
 
   int x = blockIdx.x;
   const int hk = x % a.Hk, place = x / a.Hk;
@@ -202,7 +214,7 @@ __global__ __launch_bounds__(256, 2) void lf_packed_dkv_kernel(PackedArgs a) {
   const Span s = span_of(a, b);
   const int j0 = tile * kTokens;
   if (tile < 0 || j0 >= s.nk) return;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((threadIdx.x >> 6) & 3);
   const int ln = lane & 31, kg = lane >> 5, rh = wave & 1;
   const bool is_ds = wave >= 2;
   const int j = j0 + 32 * rh + ln;
@@ -211,7 +223,8 @@ __global__ __launch_bounds__(256, 2) void lf_packed_dkv_kernel(PackedArgs a) {
   // the first rows that see this lane's token, the wavefront's last one and the workgroup's first one
   const int from = first_row(s, a.unit, j), from_last = first_row(s, a.unit, min(j0 + 32 * rh + 31, s.nk - 1));
   const int i_first = first_row(s, a.unit, j0) / kTile * kTile;
-  const int tiles = i_first < s.nq ? (s.nq - i_first + kTile - 1) / kTile : 0, steps_all = tiles;
+  const int tiles = i_first < s.nq ? (s.nq - i_first + kTile - 1) / kTile : 0;
+  const int steps_all = tiles * a.G, steps = (steps_all + SPLIT - 1) / SPLIT, step0 = group * steps;    // this group's: [step0, step0 + steps), of all heads
 
   Frag of[KS];
   {
@@ -233,9 +246,10 @@ __global__ __launch_bounds__(256, 2) void lf_packed_dkv_kernel(PackedArgs a) {
   const uint32_t st_off = (uint32_t)lane * 4u;
   const float* stat = is_ds ? a.ndelta : a.lse2;
   // where the next request goes: rows [ri, ri + 32) of the sequence, head rg of the group
-  int ri = i_first, rg = 0;
+  int ri = tiles > 0 ? i_first + step0 % tiles * kTile : 0, rg = tiles > 0 ? step0 / tiles : 0;
+  const int wi0 = ri;
   auto request = [&](int to) __attribute__((always_inline)) {
-    const int h = hk * a.G + rg, n = min(kTile, s.nq - ri);
+    const int h = hk * a.G + min(rg, a.G - 1), n = rg < a.G ? min(kTile, s.nq - ri) : 0;
     const int64_t first = (int64_t)s.q0 + ri;
     fetch<LPW>(rows_rsrc(a.Q + (int64_t)h * a.q_head, first, n, q_row), lds_addr(buf[to] + LPW * 64 * wave), qoff);
     fetch<LPW>(rows_rsrc(a.dO + (int64_t)h * a.o_head, first, n, o_row), lds_addr(buf[to] + T32 + LPW * 64 * wave), ooff);
@@ -304,6 +318,7 @@ __global__ __launch_bounds__(256, 2) void lf_packed_dkv_kernel(PackedArgs a) {
   f32x16 dp_prev = zero16();
   // role 0, step t: rows [i, i + 32)
   auto p_step = [&](int t, int at, int i) __attribute__((always_inline)) {
+    const bool none = SPLIT > 1 && step0 + t >= steps_all;
     Frag f[KS];
     rows_of(buf[at], f);
     const f32x16 lse = stats16(at);
@@ -312,11 +327,11 @@ __global__ __launch_bounds__(256, 2) void lf_packed_dkv_kernel(PackedArgs a) {
     bf16x8 tf[MB];
     first_half(buf[at] + T32, tf);
     __builtin_amdgcn_sched_barrier(0);
-    if (i < from_last || i + kTile > s.nq) {        // (rows behind the last one were loaded as zeros, their statistics too)
+    if (i < from_last || i + kTile > s.nq || none) {        // (rows behind the last one were loaded as zeros, their statistics too)
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
         const int r = i + 8 * (e >> 2) + 4 * kg + (e & 3);
-        if (r < from || r >= s.nq) sc[e] = -INFINITY;
+        if (r < from || r >= s.nq || none) sc[e] = -INFINITY;
       }
     }
     bf16x8 pf[2];
@@ -344,8 +359,7 @@ __global__ __launch_bounds__(256, 2) void lf_packed_dkv_kernel(PackedArgs a) {
     pu[0] = ph[t & 1][rh][0][lane];
     pu[1] = ph[t & 1][rh][1][lane];
   };
-  const int steps = steps_all * a.G;
-  int wi = i_first, wp = i_first;   // rows of the present step, and of the one before
+  int wi = wi0, wp = wi0;           // rows of the present step, and of the one before
   if (steps > 0) {
     request(0);
     __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
@@ -401,6 +415,35 @@ __global__ __launch_bounds__(256, 2) void lf_packed_dkv_kernel(PackedArgs a) {
       ds_finish(prv, wi, pu, tf);
     }
   }
+  if constexpr (SPLIT > 1) {
+    // the other groups leave their sums where the tiles were (none is on its way any more), the first adds them to its own
+    constexpr int N = MB * 4 * 64;
+    static_assert((SPLIT - 1) * 4 * N <= SPLIT * 3 * 2 * T32, "the sums fit the stages");
+    f32x4* const sums = reinterpret_cast<f32x4*>(&buf_all[0][0][0]);
+    f32x4* const mine = sums + ((group - 1) * 4 + wave) * N;
+    __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+    __syncthreads();
+    if (group > 0) {
+#pragma unroll
+      for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) mine[(4 * mb + g) * 64 + lane] = f32x4{acc[mb][4 * g], acc[mb][4 * g + 1], acc[mb][4 * g + 2], acc[mb][4 * g + 3]};
+    }
+    __syncthreads();
+    if (group > 0) return;
+#pragma unroll
+    for (int o = 1; o < SPLIT; ++o) {
+      const f32x4* theirs = sums + ((o - 1) * 4 + wave) * N;
+#pragma unroll
+      for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const f32x4 y = theirs[(4 * mb + g) * 64 + lane];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[mb][4 * g + e] += y[e];
+        }
+    }
+  }
   if (!ok) return;
   uint16_t* op = is_ds ? a.dK + (int64_t)hk * a.k_head + token * a.k_tok : a.dV + (int64_t)hk * a.v_head + token * a.v_tok;
   const float factor = is_ds ? a.scale : 1.0f;
@@ -420,12 +463,16 @@ template <int D> int launch(const PackedArgs& a, hipStream_t st) {
     PackedArgs q = a;
     q.slots = a.q_len / 128 + a.seqs;
     const dim3 grid((unsigned)((int64_t)q.slots * a.H));
-    if (lf_launch(lf_packed_dq_kernel<D, true>, grid, dim3(256), 0, st, q) != hipSuccess) return LF_ERR_HIP;
-    if (lf_launch(lf_packed_dq_kernel<D, false>, grid, dim3(256), 0, st, q) != hipSuccess) return LF_ERR_HIP;
+    if (lf_launch(lf_packed_dq_kernel<D>, grid, dim3(256), 0, st, q) != hipSuccess) return LF_ERR_HIP;
   }
   if (a.kv_len == 0) return LF_OK;
   if (D == 128 && (int64_t)a.kv_len * a.Hk >= (int64_t)256 * 128) return lf_launch_packed_dkv_wide(a, st);
-  return lf_launch(lf_packed_dkv_kernel<D>, dim3((unsigned)((int64_t)(a.kv_len / 64 + a.seqs) * a.Hk)), dim3(256), 0, st, a) == hipSuccess ? LF_OK : LF_ERR_HIP;
+  constexpr int kSplit = D == 128 ? 2 : 4;       // groups that a compute unit's LDS has room for
+  const int64_t blocks = (int64_t)(a.kv_len / 64 + a.seqs) * a.Hk;
+  const bool split = (int64_t)a.kv_len * a.Hk <= 64 * 256;
+  const hipError_t rc = split ? lf_launch(lf_packed_dkv_kernel<D, kSplit>, dim3((unsigned)blocks), dim3(256 * kSplit), 0, st, a)
+                              : lf_launch(lf_packed_dkv_kernel<D, 1>, dim3((unsigned)blocks), dim3(256), 0, st, a);
+  return rc == hipSuccess ? LF_OK : LF_ERR_HIP;
 }
 
 }  // namespace

@@ -190,7 +190,11 @@ __global__ __launch_bounds__(256, 1) void lf_packed_dkv_wide_kernel(PackedArgs a
       // exponential v of 32: values 0 .. 7 of both halves, then 8 .. 15
       auto prob = [&](int v) __attribute__((always_inline)) {
         const int u = v >> 4, hh = (v >> 3) & 1, e = 8 * u + (v & 7);
-        S[hh][e] = __builtin_amdgcn_exp2f(S[hh][e] * a.c);
+        float y = S[hh][e] * a.c;
+        asm volatile("" : "+v"(y));         // stays in its slot
+        y = __builtin_amdgcn_exp2f(y);
+        asm volatile("" : "+v"(y));
+        S[hh][e] = y;
         if (v & 1) {
           const bf16x2 p = {(__bf16)S[hh][e - 1], (__bf16)S[hh][e]};
           pk[hh][u][(v & 7) >> 1] = __builtin_bit_cast(uint32_t, p);
@@ -201,7 +205,9 @@ __global__ __launch_bounds__(256, 1) void lf_packed_dkv_wide_kernel(PackedArgs a
         dP[hh][e] *= S[hh][e];
         if (v & 1) {
           const bf16x2 p = {(__bf16)dP[hh][e - 1], (__bf16)dP[hh][e]};
-          ds[hh][u][(v & 7) >> 1] = __builtin_bit_cast(uint32_t, p);
+          uint32_t w = __builtin_bit_cast(uint32_t, p);
+        asm volatile("" : "+v"(w));
+        ds[hh][u][(v & 7) >> 1] = w;
         }
       };
       // dP, with 24 of the 32 exponentials
