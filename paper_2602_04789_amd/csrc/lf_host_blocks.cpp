@@ -205,7 +205,7 @@ lf_packed_plan lf_plan_packed(const lf_packed_shape* s) {
   // the longest sequence is taken to be four times the mean one
   const int64_t longest = s->kv_len < 4 * mean ? s->kv_len : 4 * mean;
   int64_t parts = (longest + each - 1) / each;
-  if (longest <= 1024) parts = 1;
+  if (longest <= 1024 || s->q_len == 0) parts = 1;
   if (parts < 1) parts = 1;
   if (parts > LF_PACKED_MAX_PARTS) parts = LF_PACKED_MAX_PARTS;
   p.parts = (int)parts;
