@@ -7,6 +7,7 @@ error status, an exception is raised.
 """
 from __future__ import annotations
 
+import array
 import ctypes as C
 import os
 from typing import Optional, Tuple
@@ -841,51 +842,48 @@ def lf_token_attn_kvq(Q, cache, capacity: int, cached_len: int, K=None, V=None, 
     return O
 
 
-_stream_dtypes = None      # torch type -> lf_dtype, for streams and gradients
+_stream_dtypes = {}        # torch type -> lf_dtype, for streams and gradients (filled once a tensor has been seen)
 
 
-def _dtype_of(t, name: str) -> int:
-    global _stream_dtypes
-    if _stream_dtypes is None:
+def _dtypes():
+    if not _stream_dtypes:
         torch = _torch or _get_torch()
-        _stream_dtypes = {torch.bfloat16: LF_BF16, torch.float32: LF_F32}
-    try:
-        return _stream_dtypes[t.dtype]
-    except KeyError:
-        raise ValueError(f"{name} must be bfloat16 or float32") from None
+        _stream_dtypes.update({torch.bfloat16: LF_BF16, torch.float32: LF_F32})
+    return _stream_dtypes
 
 
-def _row_stride(t, shape, dtype, name: str) -> int:
-    """Row stride of a [L, C] tensor with contiguous channels; that of a single row does not matter."""
-    st = t.stride()
-    if t.shape != shape or len(st) != 2 or t.dtype is not dtype or (st[1] != 1 and shape[1] != 1):
-        raise ValueError(f"{name} must be {dtype} {list(shape)} with contiguous channels")
-    return st[0] if shape[0] != 1 else shape[1]
+def _row_stride(t, shape, dtype, at: int, name: str) -> int:
+    """Row stride of a [L, C] tensor on device `at` with contiguous channels; that of a single row does not matter."""
+    if t.dtype is dtype and t.shape == shape:
+        if t.get_device() != at:
+            raise ValueError("all tensors must live on the current device")
+        st = t.stride()
+        if st[1] == 1 or shape[1] == 1:
+            return st[0] if shape[0] != 1 else shape[1]
+    raise ValueError(f"{name} must be {dtype} {list(shape)} with contiguous channels")
 
 
-def _norm_call(L, C_, dtype, kind, eps, residual_scale, gate, post_weight, weight, scale, shift, starts, group_len):
-    """(shape of the call, its groups); the row strides are still to be set."""
-    torch = _torch or _get_torch()
-    f32 = torch.float32
-    group_len, kind = _int32(group_len, kind)
-    if (starts is None) == (group_len <= 0):
-        raise ValueError("groups are given by group_len > 0 or by starts")
-    if starts is not None:
-        if starts.dtype is not torch.int32 or starts.dim() != 1 or not starts.is_contiguous() or starts.shape[0] < 2:
-            raise ValueError("starts must be contiguous int32 [groups + 1]")
+def _vector(t, n: int, dtype, at: int, name: str) -> int:
+    """Address of a contiguous tensor of n elements on device `at`."""
+    if t.dtype is not dtype or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous {dtype} [{n}]")
+    if t.get_device() != at:
+        raise ValueError("all tensors must live on the current device")
+    return t.data_ptr()
+
+
+def _norm_groups(L: int, group_len: int, starts, at: int):
+    """(groups, group_len, address of starts)"""
+    group_len, = _int32(group_len)
+    if starts is None:
+        if group_len > 0:
+            return -(-L // group_len), group_len, None
+    elif group_len <= 0:
+        if starts.dim() != 1 or starts.shape[0] < 2:
+            raise ValueError("starts must be [groups + 1]")
         groups = starts.shape[0] - 1
-    else:
-        groups = -(-L // group_len)
-    for t, name in ((post_weight, "post_weight"), (weight, "weight")):
-        if t is not None and (t.dtype is not f32 or t.shape != (C_,) or not t.is_contiguous()):
-            raise ValueError(f"{name} must be contiguous float32 [channels]")
-    strides = [C_ if t is None else _row_stride(t, (groups, C_), f32, name)
-               for t, name in ((gate, "gate"), (scale, "scale"), (shift, "shift"))]
-    return lf_norm_shape(L, C_, groups, group_len, dtype, kind, float(eps), float(residual_scale), C_, C_, C_, C_, *strides), groups
-
-
-def _ptr(t):
-    return None if t is None else t.data_ptr()
+        return groups, 0, _vector(starts, groups + 1, (_torch or _get_torch()).int32, at, "starts")
+    raise ValueError("groups are given by group_len > 0 or by starts")
 
 
 def lf_gate_norm(X, B=None, gate=None, post_weight=None, weight=None, scale=None, shift=None, group_len: int = 0, starts=None,
@@ -894,25 +892,39 @@ def lf_gate_norm(X, B=None, gate=None, post_weight=None, weight=None, scale=None
     shift; returns (Xout, Y).  X [L, C] bfloat16 or float32, B [L, C] and Y bfloat16; gate, scale and shift float32 [groups, C], one row for ``group_len``
     tokens or for the tokens [starts[g], starts[g + 1]) (int32, device); without B, Xout is X.  Xout may be X itself."""
     torch = _torch or _get_torch()
-    if X.dim() != 2:
-        raise ValueError("X must be [L, C]")
-    L, C_ = X.shape
-    p, _ = _norm_call(L, C_, _dtype_of(X, "X"), kind, eps, residual_scale, gate, post_weight, weight, scale, shift, starts, group_len)
+    bf, f32 = torch.bfloat16, torch.float32
+    rows, dtype = X.shape, X.dtype
+    if len(rows) != 2 or dtype not in (_stream_dtypes or _dtypes()):
+        raise ValueError("X must be bfloat16 or float32 [L, C]")
+    L, n = rows
     at, st = _here(stream)
-    p.x_stride = _row_stride(X, (L, C_), X.dtype, "X")
+    groups, group_len, starts_ptr = _norm_groups(L, group_len, starts, at)
+    xs = _row_stride(X, rows, dtype, at, "X")
+    xos = bs = gs = cs = hs = n
+    b_ptr = xo_ptr = gate_ptr = post_ptr = weight_ptr = scale_ptr = shift_ptr = None
     if B is not None:
-        p.b_stride = _row_stride(B, (L, C_), torch.bfloat16, "B")
+        bs, b_ptr = _row_stride(B, rows, bf, at, "B"), B.data_ptr()
         if Xout is None:
-            Xout = _new(stream, X.new_empty, (L, C_))
-        p.xo_stride = _row_stride(Xout, (L, C_), X.dtype, "Xout")
+            Xout = _new(stream, X.new_empty, rows)
+        xos, xo_ptr = _row_stride(Xout, rows, dtype, at, "Xout"), Xout.data_ptr()
+        if gate is not None:
+            gs, gate_ptr = _row_stride(gate, (groups, n), f32, at, "gate"), gate.data_ptr()
+        if post_weight is not None:
+            post_ptr = _vector(post_weight, n, f32, at, "post_weight")
     elif gate is not None or post_weight is not None or Xout is not None:
         raise ValueError("gate, post_weight and Xout go with B")
+    if weight is not None:
+        weight_ptr = _vector(weight, n, f32, at, "weight")
+    if scale is not None:
+        cs, scale_ptr = _row_stride(scale, (groups, n), f32, at, "scale"), scale.data_ptr()
+    if shift is not None:
+        hs, shift_ptr = _row_stride(shift, (groups, n), f32, at, "shift"), shift.data_ptr()
     if Y is None:
-        Y = _new(stream, X.new_empty, (L, C_), dtype=torch.bfloat16)
-    p.y_stride = _row_stride(Y, (L, C_), torch.bfloat16, "Y")
-    _one_device(at, [t for t in (X, B, gate, post_weight, weight, scale, shift, starts, Xout, Y) if t is not None])
-    rc = (_lib or load()).lf_gate_norm(X.data_ptr(), _ptr(B), _ptr(gate), _ptr(post_weight), _ptr(weight), _ptr(scale), _ptr(shift), _ptr(starts),
-                                       C.byref(p), _ptr(Xout), Y.data_ptr(), st)
+        Y = _new(stream, X.new_empty, rows, dtype=bf)
+    ys = _row_stride(Y, rows, bf, at, "Y")
+    kind, = _int32(kind)
+    p = lf_norm_shape(L, n, groups, group_len, _stream_dtypes[dtype], kind, eps, residual_scale, xs, xos, bs, ys, gs, cs, hs)
+    rc = (_lib or load()).lf_gate_norm(X.data_ptr(), b_ptr, gate_ptr, post_ptr, weight_ptr, scale_ptr, shift_ptr, starts_ptr, C.byref(p), xo_ptr, Y.data_ptr(), st)
     if rc != LF_OK:
         raise LfError(rc, "lf_gate_norm")
     return (X if B is None else Xout), Y
@@ -932,55 +944,77 @@ def lf_gate_norm_bwd(Xout, dY, dXout=None, B=None, gate=None, post_weight=None, 
     the tables' gradients float32 [groups, C] and [C], None for what the call does not have (dscale and dshift are always there)."""
     torch = _torch or _get_torch()
     bf, f32 = torch.bfloat16, torch.float32
-    if Xout.dim() != 2:
-        raise ValueError("Xout must be [L, C]")
-    L, C_ = Xout.shape
-    p, groups = _norm_call(L, C_, _dtype_of(Xout, "Xout"), kind, eps, residual_scale, gate, post_weight, weight, scale, None, starts, group_len)
+    rows, dtype = Xout.shape, Xout.dtype
+    if len(rows) != 2 or dtype not in (_stream_dtypes or _dtypes()):
+        raise ValueError("Xout must be bfloat16 or float32 [L, C]")
+    L, n = rows
     at, st = _here(stream)
-    p.xo_stride = _row_stride(Xout, (L, C_), Xout.dtype, "Xout")
+    groups, group_len, starts_ptr = _norm_groups(L, group_len, starts, at)
+    xos = _row_stride(Xout, rows, dtype, at, "Xout")
+    bs = ys = gs = cs = n
+    b_ptr = db_ptr = gate_ptr = post_ptr = weight_ptr = scale_ptr = dy_ptr = dxo_ptr = None
     if dY is not None:
-        p.y_stride = _row_stride(dY, (L, C_), bf, "dY")
-    if dXout is not None and _row_stride(dXout, (L, C_), Xout.dtype, "dXout") != p.xo_stride:
-        raise ValueError("dXout must have the strides of Xout")
+        ys, dy_ptr = _row_stride(dY, rows, bf, at, "dY"), dY.data_ptr()
+    if dXout is not None:
+        if _row_stride(dXout, rows, dtype, at, "dXout") != xos:
+            raise ValueError("dXout must have the strides of Xout")
+        dxo_ptr = dXout.data_ptr()
     if dX is None:
-        dX = _new(stream, torch.empty_strided, (L, C_), (p.xo_stride, 1), dtype=Xout.dtype, device=Xout.device)
-    if _row_stride(dX, (L, C_), Xout.dtype, "dX") != p.xo_stride:
+        dX = _new(stream, torch.empty_strided, rows, (xos, 1), dtype=dtype, device=Xout.device)
+    if dX is not dXout and _row_stride(dX, rows, dtype, at, "dX") != xos:
         raise ValueError("dX must have the strides of Xout")
+    tables = 2
     if B is not None:
-        p.b_stride = _row_stride(B, (L, C_), bf, "B")
+        bs, b_ptr = _row_stride(B, rows, bf, at, "B"), B.data_ptr()
         if dB is None:
-            dB = _new(stream, torch.empty_strided, (L, C_), (p.b_stride, 1), dtype=bf, device=B.device)
-        if _row_stride(dB, (L, C_), bf, "dB") != p.b_stride:
+            dB = _new(stream, torch.empty_strided, rows, (bs, 1), dtype=bf, device=B.device)
+        if _row_stride(dB, rows, bf, at, "dB") != bs:
             raise ValueError("dB must have the strides of B")
+        db_ptr = dB.data_ptr()
+        if gate is not None:
+            gs, gate_ptr, tables = _row_stride(gate, (groups, n), f32, at, "gate"), gate.data_ptr(), 3
+        if post_weight is not None:
+            post_ptr = _vector(post_weight, n, f32, at, "post_weight")
     elif gate is not None or post_weight is not None or dB is not None:
         raise ValueError("gate, post_weight and dB go with B")
-    _one_device(at, [t for t in (Xout, dY, dXout, B, gate, post_weight, weight, scale, starts, dX, dB) if t is not None])
-    new = lambda there, *shape: _new(stream, Xout.new_empty, shape, dtype=f32) if there else None
-    dgate, dscale, dshift = new(gate is not None, groups, C_), new(True, groups, C_), new(True, groups, C_)
-    dpost, dweight = new(post_weight is not None, C_), new(weight is not None, C_)
+    if weight is not None:
+        weight_ptr = _vector(weight, n, f32, at, "weight")
+    if scale is not None:
+        cs, scale_ptr = _row_stride(scale, (groups, n), f32, at, "scale"), scale.data_ptr()
+    # the tables' gradients are parts of one tensor: an allocation instead of three
+    made = _new(stream, Xout.new_empty, (tables, groups, n), dtype=f32)
+    dscale, dshift, *more = made.unbind(0)
+    dgate = more[0] if more else None
+    dpost = None if post_ptr is None else _new(stream, Xout.new_empty, (n,), dtype=f32)
+    dweight = None if weight_ptr is None else _new(stream, Xout.new_empty, (n,), dtype=f32)
+    size = 4 * groups * n
+    base = made.data_ptr()
+    kind, = _int32(kind)
+    p = lf_norm_shape(L, n, groups, group_len, _stream_dtypes[dtype], kind, eps, residual_scale, xos, xos, bs, ys, gs, cs, n)
     lib = _lib or load()
     ws = _workspace(workspace, lambda: lib.lf_gate_norm_bwd_workspace_bytes(C.byref(p)), Xout, stream, at)
-    rc = lib.lf_gate_norm_bwd(Xout.data_ptr(), _ptr(B), _ptr(gate), _ptr(post_weight), _ptr(weight), _ptr(scale), _ptr(starts), C.byref(p), _ptr(dY),
-                              _ptr(dXout), dX.data_ptr(), _ptr(dB), _ptr(dgate), _ptr(dpost), _ptr(dweight), _ptr(dscale), _ptr(dshift),
-                              *_bytes_of(ws), st)
+    rc = lib.lf_gate_norm_bwd(Xout.data_ptr(), b_ptr, gate_ptr, post_ptr, weight_ptr, scale_ptr, starts_ptr, C.byref(p), dy_ptr, dxo_ptr, dX.data_ptr(), db_ptr,
+                              base + 2 * size if more else None, None if dpost is None else dpost.data_ptr(), None if dweight is None else dweight.data_ptr(),
+                              base, base + size, *_bytes_of(ws), st)
     if rc != LF_OK:
         raise LfError(rc, "lf_gate_norm_bwd")
     return dX, dB, dgate, dpost, dweight, dscale, dshift
 
 
 def _packed(Q, K, V, O, q_start, kv_start, causal):
-    """(shape of the call, its tensors) for [H, L, d] tensors."""
-    torch = _torch or _get_torch()
+    """The shape of a call with [H, L, d] tensors."""
+    i32 = (_torch or _get_torch()).int32
     (qsh, qt, qh), (ksh, kt, kh), (vsh, vt, vh), (osh, ot, oh) = _rows(Q, "Q"), _rows(K, "K"), _rows(V, "V"), _rows(O, "O")
-    if ksh != vsh or ksh[2] != qsh[2] or osh != qsh:
+    heads, q_len, d = qsh
+    kv_heads, kv_len, kd = ksh
+    if ksh != vsh or kd != d or osh != qsh:
         raise ValueError("K and V must be [kv_heads, kv_len, d], O [heads, q_len, d] as Q")
-    for t, name in ((q_start, "q_start"), (kv_start, "kv_start")):
-        if t.dtype is not torch.int32 or t.dim() != 1 or not t.is_contiguous() or t.shape[0] < 2:
-            raise ValueError(f"{name} must be contiguous int32 [seqs + 1]")
-    if q_start.shape != kv_start.shape:
-        raise ValueError("q_start and kv_start must have one length")
-    causal, q_len, kv_len = _int32(causal, qsh[1], ksh[1])
-    return lf_packed_shape(qsh[0], ksh[0], qsh[2], q_start.shape[0] - 1, q_len, kv_len, causal, LF_BF16, qt, qh, kt, kh, vt, vh, ot, oh)
+    n = q_start.shape
+    if q_start.dtype is not i32 or kv_start.dtype is not i32 or len(n) != 1 or n[0] < 2 or kv_start.shape != n or not q_start.is_contiguous() \
+            or not kv_start.is_contiguous():
+        raise ValueError("q_start and kv_start must be contiguous int32 [seqs + 1]")
+    causal, q_len, kv_len = _int32(causal, q_len, kv_len)
+    return lf_packed_shape(heads, kv_heads, d, n[0] - 1, q_len, kv_len, causal, LF_BF16, qt, qh, kt, kh, vt, vh, ot, oh)
 
 
 def _packed_sizes(query, heads, kv_heads, head_dim, seqs, q_len, kv_len, causal) -> int:
@@ -994,23 +1028,25 @@ def lf_packed_attn_workspace_bytes(heads: int, kv_heads: int, head_dim: int, seq
 
 
 def _packed_fwd(Q, K, V, q_start, kv_start, causal, softmax_scale, O, lse2, with_lse, workspace, stream, where):
-    torch = _torch or _get_torch()
     at, st = _here(stream)
     if O is None:
         O = _new(stream, Q.new_empty, Q.shape)
     p = _packed(Q, K, V, O, q_start, kv_start, causal)
+    l_ptr = None
     if with_lse:
+        f32 = (_torch or _get_torch()).float32
         if lse2 is None:
-            lse2 = _new(stream, Q.new_empty, Q.shape[:2], dtype=torch.float32)
-        if lse2.dtype is not torch.float32 or lse2.shape != Q.shape[:2] or not lse2.is_contiguous():
+            lse2 = _new(stream, Q.new_empty, Q.shape[:2], dtype=f32)
+        if lse2.dtype is not f32 or lse2.shape != Q.shape[:2] or not lse2.is_contiguous():
             raise ValueError("lse2 must be a contiguous float32 GPU tensor [heads, q_len]")
         _one_device(at, (Q, K, V, O, q_start, kv_start, lse2))
+        l_ptr = lse2.data_ptr()
     else:
         _one_device(at, (Q, K, V, O, q_start, kv_start))
     lib = _lib or load()
     ws = _workspace(workspace, lambda: lib.lf_packed_attn_workspace_bytes(C.byref(p)), Q, stream, at)
-    rc = lib.lf_packed_attn(Q.data_ptr(), K.data_ptr(), V.data_ptr(), C.byref(p), q_start.data_ptr(), kv_start.data_ptr(), float(softmax_scale),
-                            O.data_ptr(), _ptr(lse2), *_bytes_of(ws), st)
+    rc = lib.lf_packed_attn(Q.data_ptr(), K.data_ptr(), V.data_ptr(), C.byref(p), q_start.data_ptr(), kv_start.data_ptr(), softmax_scale,
+                            O.data_ptr(), l_ptr, *_bytes_of(ws), st)
     if rc != LF_OK:
         raise LfError(rc, where)
     return O, lse2
@@ -1039,7 +1075,7 @@ def lf_packed_attn_bwd(Q, K, V, O, dO, lse2, q_start, kv_start, causal: int = 0,
     torch = _torch or _get_torch()
     at, st = _here(stream)
     p = _packed(Q, K, V, O, q_start, kv_start, causal)
-    if _rows(dO, "dO")[0] != O.shape or (dO.stride() != O.stride() and _rows(dO, "dO")[1:] != (p.o_stride_tok, p.o_stride_head)):
+    if dO.shape != O.shape or dO.dtype is not torch.bfloat16 or (dO.stride() != O.stride() and _rows(dO, "dO")[1:] != (p.o_stride_tok, p.o_stride_head)):
         raise ValueError("dO must have the shape and strides of O")
     if lse2.dtype is not torch.float32 or lse2.shape != Q.shape[:2] or not lse2.is_contiguous():
         raise ValueError("lse2 must be a contiguous float32 GPU tensor [heads, q_len]")
@@ -1047,7 +1083,7 @@ def lf_packed_attn_bwd(Q, K, V, O, dO, lse2, q_start, kv_start, causal: int = 0,
         grads = [_new(stream, torch.empty_strided, t.shape, t.stride(), dtype=t.dtype, device=t.device) for t in (Q, K, V)]
     else:
         for g, t, name in zip(grads, (Q, K, V), ("dQ", "dK", "dV")):
-            if g.shape != t.shape or _rows(g, name)[1:] != _rows(t, name)[1:]:
+            if g.shape != t.shape or (g.stride() != t.stride() and _rows(g, name)[1:] != _rows(t, name)[1:]) or g.dtype is not torch.bfloat16:
                 raise ValueError(f"{name} must have the shape and strides of its input")
     dQ, dK, dV = grads
     _one_device(at, (Q, K, V, O, dO, lse2, q_start, kv_start, dQ, dK, dV))
@@ -1074,32 +1110,55 @@ def lf_grad_clip(grads, max_norm: float, out=None, eps: float = 1e-6, norm=None,
     same size; bfloat16 or float32), and returns the norm over all of them, float32 [1] on the device.  Where that is not finite they are not scaled;
     max_norm = inf takes the norm alone.  ``grads``: tensors of bfloat16 or float32 without holes."""
     torch = _torch or _get_torch()
+    kinds = _stream_dtypes or _dtypes()
     grads = list(grads)
-    to = grads if out is None else list(out)
-    if len(to) != len(grads):
-        raise ValueError("out must have a tensor for each gradient")
     at, st = _here(stream)
-    table, total = (lf_grad_tensor * max(len(grads), 1))(), 0
-    for i, (x, y) in enumerate(zip(grads, to)):
-        n = x.numel()
-        if x.get_device() != at or y.get_device() != at:
-            raise ValueError("all tensors must live on the current device")
-        if not x.is_contiguous() and not (x is y and _dense(x)):
-            raise ValueError("gradients must be contiguous (in place: without holes)")
-        if x is not y and (y.numel() != n or not y.is_contiguous()):
-            raise ValueError("out must be contiguous tensors of their gradients' sizes")
-        table[i] = lf_grad_tensor(x.data_ptr(), None if x is y else y.data_ptr(), n, _dtype_of(x, "a gradient"), _dtype_of(y, "out"))
-        total += n
+    # the C structures as rows of four 64-bit numbers: address, address or 0, elements, the two types (a third of the time that ctypes takes for them)
+    rows, total = array.array("q"), 0
+    try:
+        if out is None:
+            for x in grads:
+                if x.get_device() != at:
+                    raise ValueError("all tensors must live on the current device")
+                if not x.is_contiguous() and not _dense(x):
+                    raise ValueError("gradients must be contiguous (in place: without holes)")
+                n = x.numel()
+                rows.extend((x.data_ptr(), 0, n, kinds[x.dtype]))
+                total += n
+        else:
+            to = list(out)
+            if len(to) != len(grads):
+                raise ValueError("out must have a tensor for each gradient")
+            for x, y in zip(grads, to):
+                if x.get_device() != at or y.get_device() != at:
+                    raise ValueError("all tensors must live on the current device")
+                n = x.numel()
+                if y.numel() != n or not x.is_contiguous() or not y.is_contiguous():
+                    raise ValueError("gradients and out must be contiguous tensors of the same sizes")
+                rows.extend((x.data_ptr(), y.data_ptr(), n, kinds[x.dtype] | kinds[y.dtype] << 32))
+                total += n
+    except KeyError:
+        raise ValueError("gradients and out must be bfloat16 or float32") from None
     if norm is None:
-        norm = _new(stream, torch.empty, (1,), dtype=torch.float32, device=torch.device("cuda", at))
+        norm = _new(stream, torch.empty, (1,), dtype=torch.float32, device=_device(at))
     if norm.dtype is not torch.float32 or norm.numel() != 1 or norm.get_device() != at:
         raise ValueError("norm must be one float32 on the current device")
     lib = _lib or load()
-    ws = _workspace(workspace, lambda: lib.lf_grad_workspace_bytes(len(grads), total), norm, stream, at)
-    rc = lib.lf_grad_clip(table, len(grads), float(max_norm), float(eps), norm.data_ptr(), *_bytes_of(ws), st)
+    count = len(grads)
+    ws = _workspace(workspace, lambda: lib.lf_grad_workspace_bytes(count, total), norm, stream, at)
+    rc = lib.lf_grad_clip(rows.buffer_info()[0], count, float(max_norm), float(eps), norm.data_ptr(), *_bytes_of(ws), st)
     if rc != LF_OK:
         raise LfError(rc, "lf_grad_clip")
     return norm
+
+
+_devices = {}      # index -> torch.device
+
+
+def _device(at: int):
+    if at not in _devices:
+        _devices[at] = (_torch or _get_torch()).device("cuda", at)
+    return _devices[at]
 
 
 def _dense(t) -> bool:
