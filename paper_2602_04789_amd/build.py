@@ -28,6 +28,7 @@ OBJ = os.path.join(PKG, "_build")
 SOURCES = ["lf_host.cpp", "lf_select.hip", "lf_attn.hip", "lf_attn_wide.hip", "lf_attn_bwd.hip", "lf_attn_bwd_wide.hip", "lf_attn_bwd_q_wide.hip",
            "lf_producer.hip", "lf_host_rollout.cpp", "lf_rope_axes.hip", "lf_kvq.hip", "lf_kvq_attn.hip",
            "lf_host_blocks.cpp", "lf_gate_norm.hip", "lf_grad_clip.hip", "lf_packed_attn.hip", "lf_packed_rows.hip", "lf_packed_bwd.hip",
+           "lf_packed_attn_wide.hip",
            "lf_packed_dkv_wide.hip"]
 COMMON = ["-O3", "-std=c++17", "-fPIC", "-I", os.path.join(ROOT, "include"), "-I", CSRC,
           "-Wall", "-Wno-unused-function"]

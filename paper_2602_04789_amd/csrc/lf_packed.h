@@ -23,6 +23,7 @@ struct PackedArgs {
 };
 
 PackedArgs lf_packed_args(const lf_packed_call* c);
+int lf_launch_packed_attn_wide(PackedArgs a, hipStream_t st);
 int lf_launch_packed_dkv_wide(const PackedArgs& a, hipStream_t st);
 int lf_launch_packed_join(const PackedArgs& a, int d, int tile_rows, bool few, hipStream_t st);
 

@@ -293,6 +293,11 @@ int lf_launch_packed_attn(const lf_packed_call* c, void* stream) {
   const PackedArgs a = lf_packed_args(c);
   const int d = c->s->head_dim;
   hipStream_t st = (hipStream_t)stream;
+  // 64 rows of a wavefront where a sequence's rows see 4096 tokens or more in the mean (us, 32 and 64 rows): 40 heads, 4680 rows of 4680 tokens 442 and 421,
+  // of 18 720 tokens 1785 and 1652; 12 heads, 4096 tokens 90 and 90, 512 tokens 16 and 24 (its start and end take 6 us more); causal, 40 heads of 4680 tokens
+  // 229 and 246, of 8192 tokens 663 and 656, of 16 384 tokens 2617 and 2522.
+  const int64_t seen = c->s->kv_len / (c->s->causal ? 2 : 1);
+  if (d == 128 && a.parts == 1 && c->s->q_len >= 512 * (int64_t)c->s->seqs && seen >= 4096 * (int64_t)c->s->seqs) return lf_launch_packed_attn_wide(a, st);
   const dim3 grid((unsigned)((int64_t)a.slots * a.H * a.parts));
   const hipError_t rc = d == 128 ? lf_launch(lf_packed_attn_kernel<128>, grid, dim3(256), 0, st, a)
                                  : lf_launch(lf_packed_attn_kernel<64>, grid, dim3(256), 0, st, a);

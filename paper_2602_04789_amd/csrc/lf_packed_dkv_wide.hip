@@ -187,28 +187,41 @@ __global__ __launch_bounds__(256, 1) void lf_packed_dkv_wide_kernel(PackedArgs a
         }
         __builtin_amdgcn_sched_barrier(0);
       }
-      // exponential v of 32: values 0 .. 7 of both halves, then 8 .. 15
-      auto prob = [&](int v) __attribute__((always_inline)) {
-        const int u = v >> 4, hh = (v >> 3) & 1, e = 8 * u + (v & 7);
-        float y = S[hh][e] * a.c;
-        asm volatile("" : "+v"(y));         // stays in its slot
-        y = __builtin_amdgcn_exp2f(y);
-        asm volatile("" : "+v"(y));
-        S[hh][e] = y;
-        if (v & 1) {
-          const bf16x2 p = {(__bf16)S[hh][e - 1], (__bf16)S[hh][e]};
-          pk[hh][u][(v & 7) >> 1] = __builtin_bit_cast(uint32_t, p);
+      // Value v of 32 (values 0 .. 7 of both halves, then 8 .. 15) is scaled at beat v, exp2 at the next and packed (odd v) at the one behind, dS a slot
+      // ahead of where it is packed: no instruction waits for the one before it.
+      float y[4];
+      auto stay = [](auto& w) __attribute__((always_inline)) { asm volatile("" : "+v"(w)); };      // in its slot
+      auto half_of = [](int v) { return (v >> 3) & 1; };
+      auto at_of = [](int v) { return 8 * (v >> 4) + (v & 7); };
+      auto beat = [&](int n) __attribute__((always_inline)) {
+        if (n >= 2 && n < 34 && (n & 1)) {
+          const int v = n - 2, hh = half_of(v);
+          const bf16x2 p = {(__bf16)S[hh][at_of(v) - 1], (__bf16)S[hh][at_of(v)]};
+          uint32_t w = __builtin_bit_cast(uint32_t, p);
+          stay(w);
+          pk[hh][v >> 4][(v & 7) >> 1] = w;
+        }
+        if (n >= 1 && n < 33) {
+          float w = __builtin_amdgcn_exp2f(y[(n - 1) & 3]);
+          stay(w);
+          S[half_of(n - 1)][at_of(n - 1)] = w;
+        }
+        if (n < 32) {
+          y[n & 3] = S[half_of(n)][at_of(n)] * a.c;
+          stay(y[n & 3]);
         }
       };
       auto grad = [&](int v) __attribute__((always_inline)) {
-        const int u = v >> 4, hh = (v >> 3) & 1, e = 8 * u + (v & 7);
-        dP[hh][e] *= S[hh][e];
-        if (v & 1) {
-          const bf16x2 p = {(__bf16)dP[hh][e - 1], (__bf16)dP[hh][e]};
-          uint32_t w = __builtin_bit_cast(uint32_t, p);
-        asm volatile("" : "+v"(w));
-        ds[hh][u][(v & 7) >> 1] = w;
-        }
+        float w = dP[half_of(v)][at_of(v)] * S[half_of(v)][at_of(v)];
+        stay(w);
+        dP[half_of(v)][at_of(v)] = w;
+      };
+      auto pack = [&](int v) __attribute__((always_inline)) {        // v odd
+        const int hh = half_of(v);
+        const bf16x2 p = {(__bf16)dP[hh][at_of(v) - 1], (__bf16)dP[hh][at_of(v)]};
+        uint32_t w = __builtin_bit_cast(uint32_t, p);
+        stay(w);
+        ds[hh][v >> 4][(v & 7) >> 1] = w;
       };
       // dP, with 24 of the 32 exponentials
 #pragma unroll
@@ -222,7 +235,7 @@ __global__ __launch_bounds__(256, 1) void lf_packed_dkv_wide_kernel(PackedArgs a
           else tlo[mb] = tread(kO + at, 0, mb, 0);
         }
 #pragma unroll
-        for (int v = n * 3 / 2; v < (n + 1) * 3 / 2; ++v) prob(v);
+        for (int v = n * 3 / 2; v < (n + 1) * 3 / 2; ++v) beat(v);
         __builtin_amdgcn_sched_barrier(0);
       }
       if (s.nk == 1 || (lone >= i && lone < i + kTile)) {
@@ -239,11 +252,16 @@ __global__ __launch_bounds__(256, 1) void lf_packed_dkv_wide_kernel(PackedArgs a
         if (n < 8) {
           if (n & 1) thi[MB + mb] = tread(kO + at, 1, mb, 1);
           else tlo[MB + mb] = tread(kO + at, 1, mb, 0);
-          prob(24 + n);
+          beat(24 + n);
+          if (n == 7) {
+            beat(32);
+            beat(33);
+          }
         } else {
           if (n & 1) uhi[mb] = tread(at, 0, mb, 1);
           else ulo[mb] = tread(at, 0, mb, 0);
         }
+        if (n > 0) pack(2 * n - 1);
         grad(2 * n);
         grad(2 * n + 1);
         __builtin_amdgcn_sched_barrier(0);
@@ -260,6 +278,7 @@ __global__ __launch_bounds__(256, 1) void lf_packed_dkv_wide_kernel(PackedArgs a
       for (int n = 0; n < 16; ++n) {
         const int u = n >> 3, mb = (n >> 1) & 3, hh = n & 1;
         accumulate(dk[hh][mb], join(ulo[u * MB + mb], uhi[u * MB + mb]), ds[hh][u]);
+        if (n == 0) pack(31);
         if (n < 8) {
           if (n & 1) uhi[MB + mb] = tread(at, 1, mb, 1);
           else ulo[MB + mb] = tread(at, 1, mb, 0);

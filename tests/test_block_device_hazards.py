@@ -6,7 +6,7 @@ import pytest
 from test_device_hazards import assembly, hazards
 
 
-@pytest.mark.parametrize("src", ["lf_packed_attn.hip", "lf_packed_rows.hip", "lf_packed_bwd.hip", "lf_packed_dkv_wide.hip"])
+@pytest.mark.parametrize("src", ["lf_packed_attn.hip", "lf_packed_attn_wide.hip", "lf_packed_rows.hip", "lf_packed_bwd.hip", "lf_packed_dkv_wide.hip"])
 def test_instructions_keep_their_distance_on_every_path(src):
     found = hazards(assembly(src))
     if src == "lf_packed_rows.hip":     # its products are the compiler's own, 16 x 16 ones of half the passes that the check counts with

@@ -163,6 +163,33 @@ def test_many_tokens_by_chunks(gpu):
     _run(gpu, 16, 16, 128, [0, 1000, 2100], [0, 1000, 2100], 300, seed=7)
 
 
+@pytest.mark.parametrize("H,Hk,q,kv,causal,layout,pad", [
+    (24, 8, [0, 700, 1400], [0, 3001, 8300], 0, "heads", 0), (32, 32, [0, 1100], [0, 8193], 1, "tokens", 8),
+    (27, 9, [3, 903, 1290], [5, 9000, 16500], 300, "heads", 24), (16, 4, [0, 1, 1, 700, 2063], [0, 4000, 4100, 12000, 16500], 0, "tokens", 0),
+    (12, 12, [0, 2100, 3074], [0, 1500, 20000], 1, "heads", 0)])
+def test_many_rows_of_many_tokens(gpu, H, Hk, q, kv, causal, layout, pad):
+    """The kernel of 64 rows a wavefront: 4096 tokens or more that a row sees in the mean.  In the last case 600 rows see nothing."""
+    _run(gpu, H, Hk, 128, q, kv, causal, seed=8, layout=layout, pad=pad, train=False)
+
+
+def test_many_rows_of_rising_logits(gpu):
+    """Keys that grow along 4200 tokens, then the same ones backwards: the reference moves at every tile, or only at the first."""
+    torch, lf = gpu
+    H, rows, n, d = 24, 1401, 4200, 128
+    g = torch.Generator().manual_seed(3)
+    u = torch.nn.functional.normalize(torch.randn(d, generator=g), dim=0)
+    Q = (11.3 * u).repeat(1, rows, 1).to(torch.bfloat16)
+    V = torch.randn((1, n, d), generator=g).to(torch.bfloat16)
+    qs, ks = torch.tensor([0, rows], dtype=torch.int32, device="cuda"), torch.tensor([0, n], dtype=torch.int32, device="cuda")
+    for order in (torch.arange(n), n - torch.arange(n)):
+        K = (order[:, None] * u * 0.19).to(torch.bfloat16)[None]
+        O = lf.lf_packed_attn(Q.cuda().expand(H, rows, d).contiguous(), K.cuda().expand(H, n, d).contiguous(), V.cuda().expand(H, n, d).contiguous(), qs, ks)
+        assert torch.equal(O, O[:1].expand_as(O))
+        ref, _, size = R.packed_attention(_np(Q[:, :1]), _np(K), _np(V), [0, 1], [0, n], 0, d ** -0.5)
+        # logits of up to 800, as below
+        _ok("O", _np(O[:1]), np.broadcast_to(ref, (1, rows, d)), np.broadcast_to(size, (1, rows, d)), 2 * HALF + 2.0 ** -7)
+
+
 def test_larger_keys_and_scales(gpu):
     """Logits of some hundreds: the reference of the softmax moves, and most probabilities vanish."""
     for d in (64, 128):
