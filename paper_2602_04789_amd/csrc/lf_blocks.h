@@ -43,10 +43,11 @@ int lf_launch_gate_norm_bwd(const lf_norm_call* c, void* stream);
 
 // ---- gradient clipping ----
 
-// Elements of a workgroup's share of a tensor.
+// Elements of a workgroup's share of a tensor: the fewest that leave about 1000 shares or less, since each one has the parts of the norm to add (18 tensors of 0.8 million
+// float32: 6.4 us, shares of 4096 7.3), and at the most 65 536 (340 million float32: 236 us; 32 768 244, 4096 377).
 inline int64_t lf_grad_chunk(int64_t numel) {
-  int64_t c = 4096;
-  while (c < 65536 && numel / c > 4096) c *= 2;
+  int64_t c = 16384;
+  while (c < 65536 && numel / c > 1024) c *= 2;
   return c;
 }
 inline int64_t lf_grad_most_chunks(int32_t count, int64_t numel) { return numel / lf_grad_chunk(numel) + count; }

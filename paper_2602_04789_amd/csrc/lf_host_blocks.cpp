@@ -92,6 +92,8 @@ float scale_or_default(float s, int d) { return s > 0.0f ? s : 1.0f / sqrtf((flo
 
 }  // namespace
 
+// One chunk to a thread as far as 256 threads go (4680 rows, us, with one and with three: of 1536 14.3 and 15.9, of 2048 16.4 and 22.8), then three, which
+// four wavefronts hold up to 6144 channels, then two of sixteen.
 int lf_norm_fwd_rows(const lf_norm_shape* s, lf_norm_lay* lay) {
   const int chunks = s->channels / 8;
   *lay = lf_lay_norm(s->channels, chunks <= 256 ? 1 : chunks <= 768 ? 3 : 2);
@@ -104,9 +106,11 @@ lf_norm_slots lf_norm_bwd_slots(const lf_norm_shape* s) {
   lf_norm_slots n;
   n.waves = chunks <= 192;
   n.lay = lf_lay_norm(s->channels, n.waves ? (chunks + 63) / 64 : chunks <= 768 ? 3 : 2);
-  // as many slots as the chip has room for at once: with two or three chunks to a thread a SIMD holds one wavefront, with one three of them
+  // As many slots as the chip has room for at once: with two or three chunks to a thread a SIMD holds one wavefront (4680 rows of 1536: 40 us, two slots
+  // of a wavefront each 50); with one it holds more, and two keep the sums of the slots few (8000 rows of 512, both launches, with one, two and three: 26.9,
+  // 27.4 and 30.1 us; 32 760 rows 71.8, 65.6 and 65.9).  Wavefronts with rows of their own up to 1536 channels (4680 rows: a row for all four 45 us).
   const int waves = n.lay.threads / 64;
-  const int64_t at_once = 256 * (n.waves ? (n.lay.nc == 1 ? 3 : 1) : n.lay.nc == 3 ? 4 / waves : 1);
+  const int64_t at_once = 256 * (n.waves ? (n.lay.nc == 1 ? 2 : 1) : n.lay.nc == 3 ? 4 / waves : 1);
   if (s->group_len > 0) {
     const int64_t each = at_once / s->groups > 1 ? at_once / s->groups : 1;      // slots of a group
     n.rows = (int)((s->group_len - 1) / each + 1);
@@ -177,8 +181,13 @@ extern "C" int lf_gate_norm_bwd(const void* Xout, const void* B, const float* ga
   return lf_launch_gate_norm_bwd(&c, stream);
 }
 
-// Tiles of 16 or 32 rows where sequences have 32 rows of a head or fewer on the mean.  The tokens of a tile are divided among workgroups until there
-// are about three for each compute unit (kernels of few rows; the others two), none with fewer than 512 tokens.
+// Tiles of 16 or 32 rows where sequences have 32 rows of a head or fewer in the mean (us, with them and with tiles of 128: 16 sequences of 7500
+// tokens, 40 heads on 8 of 128, 32 rows each 225 and 254, 48 rows 308 and 294; 8 heads of 64, 600 tokens, 32 rows 21 and 31, 48 rows 33 and 32).  16
+// rows and heads as 16: 110 us, as 32 113 (64 sequences of 4000 tokens, 8 heads to one); 24 of them as 32 122, as twice 16 185.
+// The tokens of a tile are divided among workgroups as long as the chip holds them all at once: one of few rows to a compute unit (16 single rows of
+// 7500 tokens in the mean: 91 us, with two 97, with three 103), of 128 rows two (12 heads, 1536 rows over 8192 tokens: 101 us, with one 207, with three 112).
+// None has fewer than 256 tokens (one row, 40 heads on 8, 4096 tokens: 10.1 us, with 512 11.5, with 1024 13.8), of 128 rows 512 (12 heads, 512 rows,
+// 2048 tokens: 24.0 us, with 256 27.6).  512 tokens stay together, and sequences of 256 in the mean.
 lf_packed_plan lf_plan_packed(const lf_packed_shape* s) {
   lf_packed_plan p;
   const int64_t group = s->heads / s->kv_heads, rows = (int64_t)s->q_len * group;
@@ -189,7 +198,7 @@ lf_packed_plan lf_plan_packed(const lf_packed_shape* s) {
     p.slots = rows / p.tile + s->seqs;
     const int64_t full = (rows + p.tile - 1) / p.tile, some = s->q_len < s->seqs ? s->q_len : s->seqs;
     tiles = (full > some ? full : some) * s->kv_heads;
-    want = 768;
+    want = 256;
   } else {
     p.tile = 128;
     p.slots = (int64_t)s->q_len / p.tile + s->seqs;
@@ -197,15 +206,14 @@ lf_packed_plan lf_plan_packed(const lf_packed_shape* s) {
     want = tiles <= 256 ? 512 : 1;
   }
   if (tiles < 1) tiles = 1;
-  // tokens of all tiles, if every sequence has its share of them, over the workgroups wanted
-  const int64_t mean = (int64_t)s->kv_len / s->seqs;
-  int64_t each = want > 1 ? (mean * tiles / want + 63) / 64 * 64 : (int64_t)1 << 30;
-  if (each < 512) each = 512;
+  const int64_t mean = (int64_t)s->kv_len / s->seqs, least = p.few ? 256 : 512, per = want > tiles ? want / tiles : 1;
+  int64_t each = want > 1 ? ((mean + per - 1) / per + 63) / 64 * 64 : (int64_t)1 << 30;
+  if (each < least) each = least;
   if (each > 1 << 30) each = 1 << 30;
   // the longest sequence is taken to be four times the mean one
   const int64_t longest = s->kv_len < 4 * mean ? s->kv_len : 4 * mean;
   int64_t parts = (longest + each - 1) / each;
-  if (longest <= 1024 || s->q_len == 0) parts = 1;
+  if ((s->seqs == 1 ? longest : 2 * mean) <= 512 || s->q_len == 0) parts = 1;
   if (parts < 1) parts = 1;
   if (parts > LF_PACKED_MAX_PARTS) parts = LF_PACKED_MAX_PARTS;
   p.parts = (int)parts;

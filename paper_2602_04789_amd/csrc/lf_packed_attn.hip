@@ -35,7 +35,7 @@ __global__ __launch_bounds__(256, 2) void lf_packed_attn_kernel(PackedArgs a) {
   x /= a.Hk;
   const int h = hk * a.G + x % a.G;
   x /= a.G;
-  const int part = x % a.parts, place = a.slots - 1 - x / a.parts;
+  const int part = x / a.slots, place = a.slots - 1 - x % a.slots;        // (parts that a short sequence leaves empty come last)
   int tile;
   const int b = find_tile(a.q_start, a.seqs, a.q_len, 1, kRows, place, tile);
   const Span s = span_of(a, b);
@@ -238,19 +238,23 @@ __global__ __launch_bounds__(256) void lf_packed_join_kernel(PackedArgs a, int t
   float o[W];
 #pragma unroll
   for (int e = 0; e < W; ++e) o[e] = 0.0f;
-  for (int p0 = 0; p0 < parts; p0 += 8) {
-    float v[8][W];
+  auto add = [&](int p0, auto many) __attribute__((always_inline)) {         // that many parts, their loads all at once
+    constexpr int N = decltype(many)::value;
+    float v[N][W];
 #pragma unroll
-    for (int k = 0; k < 8; ++k)
+    for (int k = 0; k < N; ++k)
 #pragma unroll
-      for (int e = 0; e < W; ++e) v[k][e] = p0 + k < parts ? a.state_o[(first + (int64_t)(p0 + k) * tile_rows) * D + W * lane + e] : 0.0f;
+      for (int e = 0; e < W; ++e) v[k][e] = a.state_o[(first + (int64_t)min(p0 + k, parts - 1) * tile_rows) * D + W * lane + e];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
+    for (int k = 0; k < N; ++k) {
       const float wk = __shfl(w, p0 + k);
 #pragma unroll
-      for (int e = 0; e < W; ++e) o[e] = fmaf(wk, v[k][e], o[e]);
+      for (int e = 0; e < W; ++e) o[e] = fmaf(wk, p0 + k < parts ? v[k][e] : 0.0f, o[e]);
     }
-  }
+  };
+  if (parts > 0 && parts <= 4) add(0, std::integral_constant<int, 4>{});
+  else
+    for (int p0 = 0; p0 < parts; p0 += 16) add(p0, std::integral_constant<int, 16>{});
   const float inv = L > 0.0f ? 1.0f / L : 0.0f;
   const int64_t token = (int64_t)s.q0 + i;
   if (a.lse2 && lane == 0) a.lse2[(int64_t)h * a.q_len + token] = L > 0.0f ? M + __builtin_log2f(L) : INFINITY;

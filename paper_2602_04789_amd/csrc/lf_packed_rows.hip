@@ -36,7 +36,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void lf_packed_rows_kernel(PackedAr
   int x = blockIdx.x;
   const int hk = x % a.Hk;
   x /= a.Hk;
-  const int part = x % a.parts, place = x / a.parts;
+  const int place = x % a.slots, part = x / a.slots;      // (parts that a short sequence leaves empty come last)
   int tile;
   const int b = find_tile(a.q_start, a.seqs, a.q_len, a.G, R, place, tile);
   const Span s = span_of(a, b);

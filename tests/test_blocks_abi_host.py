@@ -125,8 +125,9 @@ def test_which_kernels_a_packed_call_takes(lib):
     """From the scratch that divided calls ask for: tiles of 16 and 32 rows and head, or of 128 rows."""
     def states(H, Hk, d, seqs, q, kv):
         return lf.lf_packed_attn_workspace_bytes(H, Hk, d, seqs, q, kv, 1) // ((d + 2) * 4)
-    assert states(12, 12, 128, 1, 1, 1024) == 0 and states(12, 12, 128, 1, 1, 1025) > 0       # short axes stay whole
-    assert states(12, 12, 128, 1, 1, 130000) == 12 * 64 * 16                                  # one tile of 16 rows a head, 64 parts
+    assert states(12, 12, 128, 1, 1, 512) == 0 and states(12, 12, 128, 1, 1, 513) > 0       # short axes stay whole
+    assert states(12, 12, 128, 1, 1, 130000) == 12 * 21 * 16                                  # one tile of 16 rows a head, 21 parts: 252 workgroups
+    assert states(3, 3, 128, 1, 1, 130000) == 3 * 64 * 16                                    # 64 parts at the most
     assert states(40, 8, 128, 16, 16, 120003) % (17 * 8 * 0 + 8 * 16) == 0
     assert states(40, 8, 128, 1, 4, 130000) % (8 * 32) == 0                                    # 20 rows and heads: tiles of 32
     assert states(1, 1, 64, 1, 33, 130000) % 128 == 0                                          # more than 32 rows

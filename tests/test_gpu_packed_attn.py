@@ -190,6 +190,28 @@ def test_many_rows_of_rising_logits(gpu):
         _ok("O", _np(O[:1]), np.broadcast_to(ref, (1, rows, d)), np.broadcast_to(size, (1, rows, d)), 2 * HALF + 2.0 ** -7)
 
 
+@pytest.mark.parametrize("H,Hk,q,kv,causal", [(9, 9, [0, 600, 600, 1401, 2100], [0, 555, 777, 1300, 2051], 0), (24, 8, [0, 1, 2, 300], [0, 1, 258, 2310], 0),
+                                              (64, 64, [0, 64, 700, 771], [0, 64, 700, 771], 1), (48, 24, [0, 1000, 2049], [0, 1000, 2049], 300)])
+def test_gradients_of_many_tokens(gpu, H, Hk, q, kv, causal):
+    """The gradient kernel of 256 tokens a workgroup: tokens x heads of 18 432 or more, 49 152 where rows see less than all."""
+    _run(gpu, H, Hk, 128, q, kv, causal, seed=9)
+
+
+@pytest.mark.parametrize("d,H,Hk,q,kv,causal", [(128, 64, 32, [0, 64, 500, 1100], [0, 64, 500, 1100], 1), (64, 64, 32, [0, 64, 500, 1100], [0, 64, 500, 1100], 0)])
+def test_gradients_of_undivided_workgroups(gpu, d, H, Hk, q, kv, causal):
+    """The gradient kernel of 64 tokens a workgroup, with enough of them for the chip."""
+    _run(gpu, H, Hk, d, q, kv, causal, seed=10)
+
+
+@pytest.mark.parametrize("seqs,rows", [(64, 32), (65, 32), (63, 33), (70, 4)])
+def test_places_of_full_tiles(gpu, seqs, rows):
+    """Sequences of whole tiles, so a place of each of them is left over; more than 64 find their tiles another way."""
+    starts = [rows * i for i in range(seqs + 1)]
+    for d, H, Hk in ((64, 2, 2), (128, 8, 1)):
+        _run(gpu, H, Hk, d, starts, [7 * i + (i // 3) * 40 for i in range(seqs + 1)], 0, seed=11, train=False)
+    _run(gpu, 2, 1, 64, [5 * rows * i for i in range(seqs + 1)], [rows * i for i in range(seqs + 1)], 0, seed=12)
+
+
 def test_larger_keys_and_scales(gpu):
     """Logits of some hundreds: the reference of the softmax moves, and most probabilities vanish."""
     for d in (64, 128):
