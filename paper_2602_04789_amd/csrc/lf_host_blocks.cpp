@@ -184,10 +184,12 @@ extern "C" int lf_gate_norm_bwd(const void* Xout, const void* B, const float* ga
 // Tiles of 16 or 32 rows where sequences have 32 rows of a head or fewer in the mean (us, with them and with tiles of 128: 16 sequences of 7500
 // tokens, 40 heads on 8 of 128, 32 rows each 225 and 254, 48 rows 308 and 294; 8 heads of 64, 600 tokens, 32 rows 21 and 31, 48 rows 33 and 32).  16
 // rows and heads as 16: 110 us, as 32 113 (64 sequences of 4000 tokens, 8 heads to one); 24 of them as 32 122, as twice 16 185.
-// The tokens of a tile are divided among workgroups as long as the chip holds them all at once: one of few rows to a compute unit (16 single rows of
-// 7500 tokens in the mean: 91 us, with two 97, with three 103), of 128 rows two (12 heads, 1536 rows over 8192 tokens: 101 us, with one 207, with three 112).
-// None has fewer than 256 tokens (one row, 40 heads on 8, 4096 tokens: 10.1 us, with 512 11.5, with 1024 13.8), of 128 rows 512 (12 heads, 512 rows,
-// 2048 tokens: 24.0 us, with 256 27.6).  512 tokens stay together, and sequences of 256 in the mean.
+// The tokens of a tile are divided among workgroups as long as the chip holds them all at once.  Of few rows a compute unit holds one: 256 for one
+// sequence (a row of 12 heads over 32 760 tokens 37 us, with 384 39, with 512 40), and half as many again for several, of which some are shorter than
+// they are taken to be (16 rows over 120 003 tokens, 40 heads on 8: sequences of uneven lengths 95 us, with 256 115, with 512 104, with 768 102; of equal ones 95, 91,
+// 97 and 103).  Of 128 rows it holds two (12 heads, 1536 rows over 8192 tokens: 101 us, with one 207, with three 112).
+// None has fewer than 512 tokens (12 heads, 512 rows over 2048 tokens: 24.0 us, with 256 27.6; 24 rows over 12 000 tokens 21.2 and 25.1), the few rows of one sequence
+// 256 (40 heads on 8, 4096 tokens: 10.1 us, with 512 11.5, with 1024 13.8).  512 tokens stay together, and sequences of 256 in the mean.
 lf_packed_plan lf_plan_packed(const lf_packed_shape* s) {
   lf_packed_plan p;
   const int64_t group = s->heads / s->kv_heads, rows = (int64_t)s->q_len * group;
@@ -198,7 +200,7 @@ lf_packed_plan lf_plan_packed(const lf_packed_shape* s) {
     p.slots = rows / p.tile + s->seqs;
     const int64_t full = (rows + p.tile - 1) / p.tile, some = s->q_len < s->seqs ? s->q_len : s->seqs;
     tiles = (full > some ? full : some) * s->kv_heads;
-    want = 256;
+    want = s->seqs == 1 ? 256 : 384;
   } else {
     p.tile = 128;
     p.slots = (int64_t)s->q_len / p.tile + s->seqs;
@@ -206,7 +208,7 @@ lf_packed_plan lf_plan_packed(const lf_packed_shape* s) {
     want = tiles <= 256 ? 512 : 1;
   }
   if (tiles < 1) tiles = 1;
-  const int64_t mean = (int64_t)s->kv_len / s->seqs, least = p.few ? 256 : 512, per = want > tiles ? want / tiles : 1;
+  const int64_t mean = (int64_t)s->kv_len / s->seqs, least = p.few && s->seqs == 1 ? 256 : 512, per = want > tiles ? want / tiles : 1;
   int64_t each = want > 1 ? ((mean + per - 1) / per + 63) / 64 * 64 : (int64_t)1 << 30;
   if (each < least) each = least;
   if (each > 1 << 30) each = 1 << 30;

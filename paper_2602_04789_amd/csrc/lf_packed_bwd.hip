@@ -11,6 +11,8 @@ namespace {
 
 constexpr int kTile = 32;         // streamed rows of a step
 
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
 // One swizzle for tiles that are read both ways (rows, and transposed: half a wavefront takes four chunks of each of four rows); the transposing
 // read of rows 8 .. 15 of 16 sees chunk bit 1 flipped where a row is 256 bytes.
 template <int CH> __device__ __forceinline__ int both_swz(int row, int ch) {
@@ -189,7 +191,8 @@ __global__ __launch_bounds__(256, 2) void lf_packed_dq_kernel(PackedArgs a) {
 }
 
 // dK and dV of 64 tokens: wavefront (rh, role) has 32 of them.  Role 0 computes S = Q K^T, P and dV^T += dO^T P, role 1 dP = dO V^T, dS and
-// dK^T += Q^T dS a step later, with the P that its partner has left in LDS; so a tile of rows lives for two steps (three stages), and one barrier a step
+// dK^T += Q^T dS a step later, with the P that its partner has left in LDS (as binary16: P is 1 at the
+// most, and dS, which is rounded to bfloat16 again, has only half a step of that to bear); so a tile of rows lives for two steps (three stages), and one barrier a step
 // is enough.  SPLIT > 1: the workgroup holds SPLIT such groups with stages of their own, each takes a share of the steps (all the same number; those past
 // the end are empty), and their sums are added through LDS in order: for calls with too few tokens to fill the chip.
 template <int D, int SPLIT>
@@ -335,10 +338,15 @@ __global__ __launch_bounds__(256 * SPLIT, SPLIT == 1 ? 2 : 1) void lf_packed_dkv
       }
     }
     bf16x8 pf[2];
+    f16x8 ps[2];
 #pragma unroll
-    for (int e = 0; e < 16; ++e) pf[e >> 3][e & 7] = (__bf16)__builtin_amdgcn_exp2f(fmaf(sc[e], a.c, -lse[e]));
-    ph[t & 1][rh][0][lane] = __builtin_bit_cast(u32x4, pf[0]);
-    ph[t & 1][rh][1][lane] = __builtin_bit_cast(u32x4, pf[1]);
+    for (int e = 0; e < 16; ++e) {
+      const float p = __builtin_amdgcn_exp2f(fmaf(sc[e], a.c, -lse[e]));
+      pf[e >> 3][e & 7] = (__bf16)p;
+      ps[e >> 3][e & 7] = (_Float16)p;
+    }
+    ph[t & 1][rh][0][lane] = __builtin_bit_cast(u32x4, ps[0]);
+    ph[t & 1][rh][1][lane] = __builtin_bit_cast(u32x4, ps[1]);
     accumulate(buf[at] + T32, tf, pf);
   };
   // the one row that sees a single token (all rows of a sequence of one token do): see the dQ kernel
@@ -350,7 +358,7 @@ __global__ __launch_bounds__(256 * SPLIT, SPLIT == 1 ? 2 : 1) void lf_packed_dkv
       for (int e = 0; e < 16; ++e)
         if (s.nk == 1 || i + 8 * (e >> 2) + 4 * kg + (e & 3) == lone) dp_prev[e] = 0.0f;
     }
-    const bf16x8 pf[2] = {__builtin_bit_cast(bf16x8, pu[0]), __builtin_bit_cast(bf16x8, pu[1])};
+    const f16x8 pf[2] = {__builtin_bit_cast(f16x8, pu[0]), __builtin_bit_cast(f16x8, pu[1])};
 #pragma unroll
     for (int e = 0; e < 16; ++e) ds[e >> 3][e & 7] = (__bf16)((float)pf[e >> 3][e & 7] * dp_prev[e]);
     accumulate(buf[at], tf, ds);
