@@ -627,10 +627,12 @@ int lf_packed_attn_bwd(const void* Q, const void* K, const void* V, const void* 
  * factor is 1: gradients in place stay as they were, and the caller sees it in `norm`.  max_norm = infinity takes the norm alone; in place nothing
  * is written where the factor is 1.
  *   tensors    host array of `count` tensors (read during the call): data and out are device memory of numel contiguous elements, LF_BF16 or LF_F32 each,
- *              aligned to their element.  out = NULL: in place, and out_dtype is not looked at.  A tensor's out overlaps no other tensor.  numel may be 0.
+ *              aligned to their element.  out = NULL: in place, and out_dtype is not looked at.  What is written overlaps no other
+ *              tensor: a gradient that is listed twice is refused, unless the norm alone is taken.  numel may be 0.
  *   norm       device, float32, one element, written (infinity above 3.4e38).
  *   workspace  device scratch of >= lf_grad_workspace_bytes(count, sum of all numel), 256-byte aligned.
- * Errors: LF_ERR_NULL; LF_ERR_SHAPE (count not in 0 .. 2^20, numel negative, more than 2^40 elements in all, max_norm or eps negative or NaN, eps infinite); LF_ERR_DTYPE;
+ * Errors: LF_ERR_NULL; LF_ERR_SHAPE (count not in 0 .. 2^20, numel negative, more than 2^40 elements in all, max_norm or eps negative or NaN, eps infinite,
+ *   a tensor that is written and overlaps another); LF_ERR_DTYPE;
  *   LF_ERR_ALIGN; LF_ERR_WORKSPACE; LF_ERR_HIP.
  */
 typedef struct {

@@ -1,6 +1,9 @@
 // Host side of the calls around the attention: validation, sizes and how a call is laid over workgroups.  No GPU code here.
 #include <math.h>
+#include <stdlib.h>
 #include <string.h>
+
+#include <algorithm>
 
 #include "lf_blocks.h"
 
@@ -89,6 +92,36 @@ int check_packed(const lf_packed_shape* s) {
 }
 bool scale_ok(float s) { return s >= 0.0f && !isinf(s); }
 float scale_or_default(float s, int d) { return s > 0.0f ? s : 1.0f / sqrtf((float)d); }
+
+// ---- gradient clipping ----
+
+struct Range {
+  uintptr_t from, to;
+  bool written;
+};
+// Whether a tensor that is written shares memory with another one (the same gradient listed twice would be scaled twice, or not).
+int written_once(const lf_grad_tensor* t, int32_t count, bool norm_alone) {
+  Range few[64], *all = 2 * (int64_t)count <= 64 ? few : (Range*)malloc(2 * (size_t)count * sizeof(Range));
+  if (!all) return LF_ERR_WORKSPACE;
+  int32_t n = 0;
+  for (int32_t i = 0; i < count; ++i) {
+    if (t[i].numel == 0) continue;
+    const uintptr_t data = (uintptr_t)t[i].data, out = (uintptr_t)t[i].out;
+    const bool apart = out && out != data;
+    all[n++] = {data, data + (uintptr_t)t[i].numel * (t[i].dtype == LF_F32 ? 4 : 2), !apart && !norm_alone};
+    if (apart) all[n++] = {out, out + (uintptr_t)t[i].numel * (t[i].out_dtype == LF_F32 ? 4 : 2), true};
+  }
+  std::sort(all, all + n, [](const Range& a, const Range& b) { return a.from < b.from; });
+  uintptr_t any = 0, written = 0;          // ends of what stands before
+  bool once = true;
+  for (int32_t i = 0; i < n && once; ++i) {
+    once = all[i].from >= (all[i].written ? any : written);
+    any = std::max(any, all[i].to);
+    if (all[i].written) written = std::max(written, all[i].to);
+  }
+  if (all != few) free(all);
+  return once ? LF_OK : LF_ERR_SHAPE;
+}
 
 }  // namespace
 
@@ -312,6 +345,8 @@ extern "C" int lf_grad_clip(const lf_grad_tensor* t, int32_t count, float max_no
     if (t[i].out == t[i].data && t[i].out_dtype != t[i].dtype) return LF_ERR_DTYPE;
     if (misaligned(t[i].data, t[i].dtype == LF_F32 ? 4 : 2) || (t[i].out && misaligned(t[i].out, t[i].out_dtype == LF_F32 ? 4 : 2))) return LF_ERR_ALIGN;
   }
+  const int rc = written_once(t, count, isinf(max_norm));
+  if (rc != LF_OK) return rc;
   if (!workspace || workspace_bytes < lf_grad_workspace_bytes(count, numel)) return LF_ERR_WORKSPACE;
   if (misaligned(norm, 4) || misaligned(workspace, 256)) return LF_ERR_ALIGN;
   return lf_launch_grad_clip(t, count, numel, max_norm, eps, norm, (double*)workspace, stream);

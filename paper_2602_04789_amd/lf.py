@@ -1108,7 +1108,7 @@ def lf_grad_workspace_bytes(count: int, numel: int) -> int:
 def lf_grad_clip(grads, max_norm: float, out=None, eps: float = 1e-6, norm=None, workspace=None, stream=None):
     """Scales gradients to a largest norm: x * min(1, max_norm / (norm + eps)), in place or into the tensors of ``out`` (one for each, of the
     same size; bfloat16 or float32), and returns the norm over all of them, float32 [1] on the device.  Where that is not finite they are not scaled;
-    max_norm = inf takes the norm alone.  ``grads``: tensors of bfloat16 or float32 without holes."""
+    max_norm = inf takes the norm alone.  ``grads``: tensors of bfloat16 or float32 without holes, each listed once."""
     torch = _torch or _get_torch()
     kinds = _stream_dtypes or _dtypes()
     grads = list(grads)

@@ -131,12 +131,15 @@ int main() {
         break;
       }
       default: {
-        lf_grad_tensor t[4];
-        const int count = PICK(0, 1, 4, 4);
+        lf_grad_tensor t[90];
+        const int count = PICK(0, 1, 4, 4, 90);
         int64_t numel = 0;
-        for (int k = 0; k < 4; ++k) {
-          t[k] = {P, rnd() % 2 ? (void*)0x20000 : nullptr, PICK(0, 1, 7, 4096, 100000, INT32_MAX, -1), PICK(0, 1, 1, 2), PICK(0, 1)};
+        const bool apart = rnd() % 4 != 0;        // or all at one place
+        for (int k = 0; k < 90; ++k) {
+          const int64_t at = apart ? (int64_t)((31 * k) % 90) << 46 : 0;
+          t[k] = {(char*)P + at, rnd() % 2 ? (char*)P + at + (apart ? (int64_t)1 << 45 : 0x10000) : nullptr, PICK(0, 1, 7, 4096, 100000, INT32_MAX, -1), PICK(0, 1, 1, 2), PICK(0, 1)};
           if (rnd() % 16 == 0) t[k].numel = stride();
+          if (k >= 4 && rnd() % 8) t[k].numel = k, t[k].dtype = 0, t[k].out_dtype = 1;
           if (k < count && t[k].numel > 0 && t[k].numel < (int64_t)1 << 41) numel += t[k].numel;
         }
         g_need = lf_grad_workspace_bytes(count, numel);

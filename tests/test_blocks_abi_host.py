@@ -155,6 +155,23 @@ def test_clipping_refuses_bad_arguments(lib):
     assert lf.lf_grad_workspace_bytes(-1, 5) == lf.lf_grad_workspace_bytes(1, -5) == lf.lf_grad_workspace_bytes(1 << 40, 5) == lf.lf_grad_workspace_bytes(1, 1 << 41) == 0
 
 
+def test_clipping_refuses_a_tensor_that_is_scaled_twice(lib):
+    """Judged from addresses; calls that are let through miss their workspace."""
+    let = lambda *e, **kw: _grads(lib, list(e), n=0, **kw) == -6
+    a, b, c = FAKE, 2 * FAKE, 3 * FAKE
+    assert let((a, None, 10, 0, 0), (b, None, 10, 0, 0)) and let((b, None, 10, 0, 0), (a, None, FAKE // 2, 0, 0)) and let((b, None, 1, 0, 0), (a, None, FAKE // 4, 1, 0))
+    assert not let((b, None, 10, 0, 0), (a, None, FAKE // 2 + 1, 0, 0)) and not let((b, None, 1, 0, 0), (a, None, FAKE // 4 + 1, 1, 0))
+    for twice in ([(a, None, 10, 0, 0)] * 2, [(a, None, 10, 0, 0), (a + 18, None, 10, 0, 0)], [(a, b, 10, 0, 0), (c, b, 10, 0, 0)], [(a, b, 10, 0, 0), (b, None, 10, 0, 0)],
+                  [(a, b, 10, 0, 0), (b, c, 10, 0, 0)], [(a, a, 10, 0, 0), (a, b, 10, 0, 0)], [(a, a + 2, 10, 0, 0)], [(a, b, FAKE // 2, 0, 1), (c - 2, None, 5, 0, 0)]):
+        assert _grads(lib, twice, n=0) == -2, twice
+        rest = [(a + (i << 32), None, 9, 0, 0) for i in range(1, 100)]
+        assert _grads(lib, rest + twice, n=0) == -2 and let(*rest)
+    assert let((a, b, 10, 0, 0), (a, c, 10, 0, 1))                                              # read twice: counted twice
+    assert let((a, None, 10, 0, 0), (a, None, 10, 0, 0), max_norm=float("inf"))                 # nothing is written
+    assert not let((a, b, 10, 0, 0), (b, None, 10, 0, 0), max_norm=float("inf"))
+    assert let((a, None, 0, 0, 0), (a, None, 10, 0, 0), (a, a, 0, 0, 0))
+
+
 def test_host_side_under_address_and_undefined_behaviour_sanitizers(tmp_path):
     """lf_host_blocks.cpp on the CPU with -fsanitize=address,undefined: sizes at and past every limit; what reaches a launcher fits its grid, its threads
     and the workspace that was asked for."""

@@ -79,6 +79,19 @@ def test_many_tensors_and_shares(gpu):
         _check(torch, x, k, f)
 
 
+@pytest.mark.parametrize("count", [1024, 1025, 2000])
+def test_more_shares_than_a_workgroup_adds(gpu, count):
+    torch, lf = gpu
+    sizes = [1 + i % 7 for i in range(count)]
+    xs, _ = _tensors(torch, sizes, "bf", seed=4)
+    keep = [x.clone() for x in xs]
+    n, f = R.clip([x.double().cpu().numpy() for x in xs], 0.5, 1e-6)
+    norm = lf.lf_grad_clip(xs, 0.5)
+    assert f < 1 and abs(float(norm) - n) <= 2.0 ** -23 * n
+    for x, k in zip(xs, keep):
+        _check(torch, x, k, f)
+
+
 def test_norm_alone(gpu):
     torch, lf = gpu
     xs, _ = _tensors(torch, [1000, 0, 77], "bf")
@@ -167,6 +180,9 @@ def test_binding_refuses(gpu):
                 dict(norm=torch.zeros(1)), dict(out=[torch.randn((5, 4), device="cuda")[:, :2]])):
         with pytest.raises(ValueError):
             lf.lf_grad_clip(**{**dict(grads=[x], max_norm=1.0), **bad})
+    with pytest.raises(lf.LfError):        # scaled twice
+        lf.lf_grad_clip([x, x], 1.0)
+    assert float(lf.lf_grad_clip([x, x], float("inf"))) > 0.0
     for bad in (dict(max_norm=-1.0), dict(max_norm=float("nan")), dict(eps=-1.0), dict(eps=float("inf")), dict(workspace=torch.empty(8, dtype=torch.uint8, device="cuda"))):
         with pytest.raises(lf.LfError):
             lf.lf_grad_clip(**{**dict(grads=[x], max_norm=1.0), **bad})
