@@ -146,7 +146,13 @@ __device__ __forceinline__ float factor_of(double sum, float max_norm, float eps
 }
 __device__ __forceinline__ double sum_parts(const double* part, int64_t parts) {
   double s = 0.0;
-  for (int64_t i = threadIdx.x; i < parts; i += kThreads) s += part[i];
+  for (int64_t i = threadIdx.x; i < parts; i += 16 * kThreads) {        // loads at once: 13 000 parts 19 us one after another
+    double v[16];
+#pragma unroll
+    for (int k = 0; k < 16; ++k) v[k] = part[min(i + k * kThreads, parts - 1)];
+#pragma unroll
+    for (int k = 0; k < 16; ++k) s += i + k * kThreads < parts ? v[k] : 0.0;
+  }
   return block_sum(s);
 }
 __global__ __launch_bounds__(kThreads) void lf_grad_norm_kernel(const double* part, int64_t parts, float max_norm, float eps, float* norm, float* factor) {

@@ -192,8 +192,8 @@ __global__ __launch_bounds__(256, 2) void lf_packed_dq_kernel(PackedArgs a) {
 
 // dK and dV of 64 tokens: wavefront (rh, role) has 32 of them.  Role 0 computes S = Q K^T, P and dV^T += dO^T P, role 1 dP = dO V^T, dS and
 // dK^T += Q^T dS a step later, with the P that its partner has left in LDS (as binary16: P is 1 at the
-// most, and dS, which is rounded to bfloat16 again, has only half a step of that to bear); so a tile of rows lives for two steps (three stages), and one barrier a step
-// is enough.  SPLIT > 1: the workgroup holds SPLIT such groups with stages of their own, each takes a share of the steps (all the same number; those past
+// most, and dS, which is rounded to bfloat16 again, has only half a step of that to bear); so one barrier a step is enough.  A tile is
+// requested two steps ahead; its Q lives for two steps (four stages), its dO for one (three).  SPLIT > 1: the workgroup holds SPLIT such groups with stages of their own, each takes a share of the steps (all the same number; those past
 // the end are empty), and their sums are added through LDS in order: for calls with too few tokens to fill the chip.
 template <int D, int SPLIT>
 __global__ __launch_bounds__(256 * SPLIT, SPLIT == 1 ? 2 : 1) void lf_packed_dkv_kernel(PackedArgs a) {
@@ -202,11 +202,12 @@ __global__ __launch_bounds__(256 * SPLIT, SPLIT == 1 ? 2 : 1) void lf_packed_dkv
   constexpr int T32 = kTile * CH;
   constexpr int LPW = T32 / 64 / 4;
   constexpr int RPI = 64 / CH;
-  __shared__ u32x4 buf_all[SPLIT][3][2 * T32];   // [step mod 3][Q | dO]
-  __shared__ f32x4 st_all[SPLIT][3][4][16];      // lse2 (role 0) or -delta of the 32 rows, for each wavefront; the upper half takes what the other lanes load
+  __shared__ u32x4 buf_all[SPLIT][7][T32];       // Q [step mod 4], dO [step mod 3]
+  __shared__ f32x4 st_all[SPLIT][3][4][16];      // [step mod 3] -lse2 / c (role 0) or -delta of the 32 rows, for each wavefront; the upper half takes what the other lanes load
   __shared__ u32x4 ph_all[SPLIT][2][2][2][64];   // P: [step parity][rh][k-step][lane]
   const int group = SPLIT > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 8) : 0;
-  u32x4 (*const buf)[2 * T32] = buf_all[group];
+  u32x4 (*const qbuf)[T32] = buf_all[group];
+  u32x4 (*const obuf)[T32] = qbuf + 4;
   f32x4 (*const st)[4][16] = st_all[group];
   u32x4 (*const ph)[2][2][64] = ph_all[group];
 
@@ -247,23 +248,26 @@ __global__ __launch_bounds__(256 * SPLIT, SPLIT == 1 ? 2 : 1) void lf_packed_dkv
     ooff[i] = (uint32_t)r * o_row + (uint32_t)both_swz<CH>(r, p) * 16u - 1024u * (i & 3);
   }
   const uint32_t st_off = (uint32_t)lane * 4u;
-  const float* stat = is_ds ? a.ndelta : a.lse2;
+  const float* stat = is_ds ? a.ndelta : a.nlse;
   // where the next request goes: rows [ri, ri + 32) of the sequence, head rg of the group
   int ri = tiles > 0 ? i_first + step0 % tiles * kTile : 0, rg = tiles > 0 ? step0 / tiles : 0;
   const int wi0 = ri;
-  auto request = [&](int to) __attribute__((always_inline)) {
+  int q_to = 0, o_to = 0;
+  auto request = [&]() __attribute__((always_inline)) {
     const int h = hk * a.G + min(rg, a.G - 1), n = rg < a.G ? min(kTile, s.nq - ri) : 0;
     const int64_t first = (int64_t)s.q0 + ri;
-    fetch<LPW>(rows_rsrc(a.Q + (int64_t)h * a.q_head, first, n, q_row), lds_addr(buf[to] + LPW * 64 * wave), qoff);
-    fetch<LPW>(rows_rsrc(a.dO + (int64_t)h * a.o_head, first, n, o_row), lds_addr(buf[to] + T32 + LPW * 64 * wave), ooff);
+    fetch<LPW>(rows_rsrc(a.Q + (int64_t)h * a.q_head, first, n, q_row), lds_addr(qbuf[q_to] + LPW * 64 * wave), qoff);
+    fetch<LPW>(rows_rsrc(a.dO + (int64_t)h * a.o_head, first, n, o_row), lds_addr(obuf[o_to] + LPW * 64 * wave), ooff);
     const int32x4 rs = aged(rows_rsrc(reinterpret_cast<const uint16_t*>(stat + (int64_t)h * a.q_len), first, n, 4u));
-    const uint32_t at = __builtin_amdgcn_readfirstlane(lds_addr(st[to][wave]));
+    const uint32_t at = __builtin_amdgcn_readfirstlane(lds_addr(st[o_to][wave]));
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" :: "s"(at), "v"(st_off), "s"(rs) : "memory", "m0");
     ri += kTile;
     if (ri >= s.nq) {
       ri = i_first;
       ++rg;
     }
+    q_to = (q_to + 1) & 3;
+    o_to = o_to == 2 ? 0 : o_to + 1;
   };
   int raddr[KS], tbase[MB];
 #pragma unroll
@@ -318,118 +322,112 @@ __global__ __launch_bounds__(256 * SPLIT, SPLIT == 1 ? 2 : 1) void lf_packed_dkv
     }
     return v;
   };
-  f32x16 dp_prev = zero16();
-  // role 0, step t: rows [i, i + 32)
-  auto p_step = [&](int t, int at, int i) __attribute__((always_inline)) {
+  // role 0, step t: rows [i, i + 32), in stages qa and at
+  auto p_step = [&](int t, int qa, int at, int i) __attribute__((always_inline)) {
     const bool none = SPLIT > 1 && step0 + t >= steps_all;
     Frag f[KS];
-    rows_of(buf[at], f);
-    const f32x16 lse = stats16(at);
+    rows_of(qbuf[qa], f);
+    f32x16 sc = stats16(at);
     __builtin_amdgcn_sched_barrier(0);
-    f32x16 sc = product(f, zero16());
+    sc = product(f, sc);
     bf16x8 tf[MB];
-    first_half(buf[at] + T32, tf);
+    first_half(obuf[at], tf);
     __builtin_amdgcn_sched_barrier(0);
     if (i < from_last || i + kTile > s.nq || none) {        // (rows behind the last one were loaded as zeros, their statistics too)
+      const int lo = none ? kTile : from - i - 4 * kg, past = s.nq - i - 4 * kg;
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        const int r = i + 8 * (e >> 2) + 4 * kg + (e & 3);
-        if (r < from || r >= s.nq || none) sc[e] = -INFINITY;
+        const int r = 8 * (e >> 2) + (e & 3);
+        if (r < lo || r >= past) sc[e] = -INFINITY;
       }
     }
     bf16x8 pf[2];
     f16x8 ps[2];
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-      const float p = __builtin_amdgcn_exp2f(fmaf(sc[e], a.c, -lse[e]));
+      const float p = __builtin_amdgcn_exp2f(sc[e] * a.c);
       pf[e >> 3][e & 7] = (__bf16)p;
       ps[e >> 3][e & 7] = (_Float16)p;
     }
     ph[t & 1][rh][0][lane] = __builtin_bit_cast(u32x4, ps[0]);
     ph[t & 1][rh][1][lane] = __builtin_bit_cast(u32x4, ps[1]);
-    accumulate(buf[at] + T32, tf, pf);
+    accumulate(obuf[at], tf, pf);
   };
   // the one row that sees a single token (all rows of a sequence of one token do): see the dQ kernel
   const int lone = a.unit == 1 ? s.nq - s.nk : -1;
-  auto ds_finish = [&](int at, int i, const u32x4 (&pu)[2], const bf16x8 (&tf)[MB]) __attribute__((always_inline)) {
-    bf16x8 ds[2];
-    if (s.nk == 1 || (lone >= i && lone < i + kTile)) {
+  // role 1, step t + 1: dS and dK of step t's rows [i, i + 32)
+  auto ds_step = [&](int t, int i, f32x16 dp) __attribute__((always_inline)) {
+    const f16x8 pf[2] = {__builtin_bit_cast(f16x8, ph[t & 1][rh][0][lane]), __builtin_bit_cast(f16x8, ph[t & 1][rh][1][lane])};
+    bf16x8 tf[MB];
+    first_half(qbuf[t & 3], tf);
+    __builtin_amdgcn_sched_barrier(0);
+    if (s.nk == 1) dp = zero16();
+    if (lone >= i && lone < i + kTile) {
+      const int r = lone - i - 4 * kg;
 #pragma unroll
       for (int e = 0; e < 16; ++e)
-        if (s.nk == 1 || i + 8 * (e >> 2) + 4 * kg + (e & 3) == lone) dp_prev[e] = 0.0f;
+        if (8 * (e >> 2) + (e & 3) == r) dp[e] = 0.0f;
     }
-    const f16x8 pf[2] = {__builtin_bit_cast(f16x8, pu[0]), __builtin_bit_cast(f16x8, pu[1])};
+    bf16x8 ds[2];
 #pragma unroll
-    for (int e = 0; e < 16; ++e) ds[e >> 3][e & 7] = (__bf16)((float)pf[e >> 3][e & 7] * dp_prev[e]);
-    accumulate(buf[at], tf, ds);
+    for (int e = 0; e < 16; ++e) ds[e >> 3][e & 7] = (__bf16)((float)pf[e >> 3][e & 7] * dp[e]);
+    accumulate(qbuf[t & 3], tf, ds);
   };
-  auto take_p = [&](int t, u32x4 (&pu)[2]) __attribute__((always_inline)) {
-    pu[0] = ph[t & 1][rh][0][lane];
-    pu[1] = ph[t & 1][rh][1][lane];
-  };
-  int wi = wi0, wp = wi0;           // rows of the present step, and of the one before
+  int wi = wi0;               // rows of the present step
   if (steps > 0) {
-    request(0);
-    __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
-    lds_barrier();
-    if (steps > 1) request(1);
-    if (!is_ds) {
-      p_step(0, 0, wi);
-    } else {
-      Frag f[KS];
-      dp_prev = stats16(0);
-      rows_of(buf[0] + T32, f);
-      dp_prev = product(f, dp_prev);
-    }
-    auto step = [&](int t, int cur, int nxt, int prv) __attribute__((always_inline)) {
-      wp = wi;
+    constexpr int kLoads = 2 * LPW + 1;       // of a request
+    // everyone's share of what was requested two steps ago has landed, and nobody reads what the next request replaces
+    auto meet = [&]() __attribute__((always_inline)) {
+      __builtin_amdgcn_s_waitcnt(vmcnt_imm(kLoads));
+      lds_barrier();
+      request();              // (past the last step: zeros, or rows of the next group)
+    };
+    request();
+    request();
+    meet();
+    // the roles meet at the same barriers
+    int cur = 0;
+    auto next = [&]() __attribute__((always_inline)) {
       wi += kTile;
       if (wi >= s.nq) wi = i_first;
-      __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
-      lds_barrier();
-      if (t + 1 < steps) request(nxt);
-      if (!is_ds) {
-        p_step(t, cur, wi);
-      } else {
-        Frag f[KS];
-        u32x4 pu[2];
-        f32x16 dp_cur = stats16(cur);
-        rows_of(buf[cur] + T32, f);
-        take_p(t - 1, pu);
-        __builtin_amdgcn_sched_barrier(0);
-        dp_cur = product(f, dp_cur);
-        bf16x8 tf[MB];
-        first_half(buf[prv], tf);
-        __builtin_amdgcn_sched_barrier(0);
-        ds_finish(prv, wp, pu, tf);
-        dp_prev = dp_cur;
-      }
-      __builtin_amdgcn_sched_barrier(0);
+      cur = cur == 2 ? 0 : cur + 1;
+      meet();
     };
-    for (int t = 1; t < steps; t += 3) {
-      step(t, 1, 2, 0);
-      if (t + 1 >= steps) break;
-      step(t + 1, 2, 0, 1);
-      if (t + 2 >= steps) break;
-      step(t + 2, 0, 1, 2);
+    if (!is_ds) {
+      p_step(0, 0, 0, wi);
+      for (int t = 1; t < steps; ++t) {
+        next();
+        p_step(t, t & 3, cur, wi);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      lds_barrier();
+    } else {
+      Frag f[KS];
+      f32x16 dp_prev = stats16(0);
+      rows_of(obuf[0], f);
+      dp_prev = product(f, dp_prev);
+      for (int t = 1; t < steps; ++t) {
+        const int wp = wi;
+        next();
+        rows_of(obuf[cur], f);
+        f32x16 dp = stats16(cur);
+        __builtin_amdgcn_sched_barrier(0);
+        dp = product(f, dp);
+        ds_step(t - 1, wp, dp_prev);
+        dp_prev = dp;
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      lds_barrier();
+      ds_step(steps - 1, wi, dp_prev);
     }
-    lds_barrier();
-    if (is_ds) {
-      u32x4 pu[2];
-      bf16x8 tf[MB];
-      const int prv = (steps - 1) % 3;
-      take_p(steps - 1, pu);
-      first_half(buf[prv], tf);
-      ds_finish(prv, wi, pu, tf);
-    }
+    __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
   }
   if constexpr (SPLIT > 1) {
     // the other groups leave their sums where the tiles were (none is on its way any more), the first adds them to its own
     constexpr int N = MB * 4 * 64;
-    static_assert((SPLIT - 1) * 4 * N <= SPLIT * 3 * 2 * T32, "the sums fit the stages");
+    static_assert((SPLIT - 1) * 4 * N <= SPLIT * 7 * T32, "the sums fit the stages");
     f32x4* const sums = reinterpret_cast<f32x4*>(&buf_all[0][0][0]);
     f32x4* const mine = sums + ((group - 1) * 4 + wave) * N;
-    __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
     __syncthreads();
     if (group > 0) {
 #pragma unroll
