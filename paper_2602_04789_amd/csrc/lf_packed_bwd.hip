@@ -472,14 +472,14 @@ template <int D> int launch(const PackedArgs& a, hipStream_t st) {
     if (lf_launch(lf_packed_dq_kernel<D>, grid, dim3(256), 0, st, q) != hipSuccess) return LF_ERR_HIP;
   }
   if (a.kv_len == 0) return LF_OK;
-  // 256 tokens of a workgroup with 72 of them or more; where rows see the tokens ahead of them only, so that the first workgroups work longest, 192
-  // (both gradients, us, with them and with the better of the two below: 12 heads of 1024 tokens 111 and 90, 1536 155 and 164, 4096 460 and 609; causal, 32
-  // heads on 4 of 8192 tokens 4174 and 3072, 12 000 7243 and 6449, 16 384 11 369 and 11 977).
-  if (D == 128 && (int64_t)a.kv_len * a.Hk >= 256 * (a.unit ? 192 : 72)) return lf_launch_packed_dkv_wide(a, st);
+  // 256 tokens of a workgroup with 112 of them or more; where rows see the tokens ahead of them only, so that the first workgroups work longest, 352
+  // (both gradients, us, with them and with the better of the two below: 12 heads of 2048 tokens 205 and 177, 2731 305 and 324; causal, 32 heads on 4 of
+  // 16 384 tokens 11 406 and 9994, 24 000 20 164 and 20 673; by chunks of 512, 12 heads of 4096 378 and 327, 8192 911 and 951).
+  if (D == 128 && (int64_t)a.kv_len * a.Hk >= 256 * (a.unit ? 352 : 112)) return lf_launch_packed_dkv_wide(a, st);
   constexpr int kSplit = D == 128 ? 2 : 4;       // groups that a compute unit's LDS has room for
   const int64_t blocks = (int64_t)(a.kv_len / 64 + a.seqs) * a.Hk;
-  // several groups to a workgroup while it has a compute unit for itself, twice over (divided and not: 32 heads on 4 of 128, 8000 tokens, causal 2977 and
-  // 3863; 8 heads of 64, 4096 tokens 340 and 369, 8192 tokens 1115 and 1087; 8 sequences of 512, 24 heads on 8 159 and 153)
+  // several groups to a workgroup while a compute unit has two of them or fewer (divided and not: 32 heads on 4 of 128, 8192 tokens, causal 2451 and
+  // 2916, 12 000 tokens 5675 and 5548; 8 heads of 64, 2048 tokens 113 and 128; 8 sequences of 512, 24 heads on 8 131 and 126)
   const bool split = (int64_t)(a.kv_len / 64 + a.seqs - 1) * a.Hk <= 2 * 256;
   const hipError_t rc = split ? lf_launch(lf_packed_dkv_kernel<D, kSplit>, dim3((unsigned)blocks), dim3(256 * kSplit), 0, st, a)
                               : lf_launch(lf_packed_dkv_kernel<D, 1>, dim3((unsigned)blocks), dim3(256), 0, st, a);
