@@ -14,11 +14,11 @@ constexpr int kTile = 32;         // streamed rows of a step
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 // One swizzle for tiles that are read both ways (rows, and transposed: half a wavefront takes four chunks of each of four rows); the transposing
-// read of rows 8 .. 15 of 16 sees chunk bit 1 flipped where a row is 256 bytes.
+// read of rows 8 .. 15 of 16 sees chunk bit 1 flipped.
 template <int CH> __device__ __forceinline__ int both_swz(int row, int ch) {
-  return CH == 16 ? ch ^ (((row & 3) << 2) | ((row >> 2) & 3)) : ch ^ ((row & 1) << 2);
+  return ch ^ (((CH == 16 ? row & 3 : (row >> 1) & 1) << 2) | ((row >> 2) & 3));
 }
-template <int CH> constexpr int kTrHiFlip = CH == 16 ? 16 : 0;
+constexpr int kTrHiFlip = 16;     // of an element's place
 
 // Rows that see this many tokens or fewer get delta = sum_y P dP (the same number) instead of dO . O: O was rounded to bfloat16, and where few
 // tokens share a row's probability, one of them nearly all of it, what that leaves in dP - delta is more than the roundings of P and dS (12
@@ -173,7 +173,7 @@ __global__ __launch_bounds__(256, 2) void lf_packed_dq_kernel(PackedArgs a) {
 #pragma unroll
       for (int mb = 0; mb < MB; ++mb) {
         const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(LDS_PTR(bf16x4, k16 + tbase[mb] + 16 * u * CH * 8));
-        const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(LDS_PTR(bf16x4, k16 + (tbase[mb] ^ kTrHiFlip<CH>) + (16 * u + 8) * CH * 8));
+        const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(LDS_PTR(bf16x4, k16 + (tbase[mb] ^ kTrHiFlip) + (16 * u + 8) * CH * 8));
         acc[mb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7), ds[u], acc[mb], 0, 0, 0);
       }
   });
@@ -287,7 +287,7 @@ __global__ __launch_bounds__(256 * SPLIT, SPLIT == 1 ? 2 : 1) void lf_packed_dkv
   auto tfrag = [&](const u32x4* at, int u, int mb) __attribute__((always_inline)) {
     const uint16_t* p = reinterpret_cast<const uint16_t*>(at);
     const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(LDS_PTR(bf16x4, p + tbase[mb] + 16 * u * CH * 8));
-    const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(LDS_PTR(bf16x4, p + (tbase[mb] ^ kTrHiFlip<CH>) + (16 * u + 8) * CH * 8));
+    const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(LDS_PTR(bf16x4, p + (tbase[mb] ^ kTrHiFlip) + (16 * u + 8) * CH * 8));
     return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
   };
   auto rows_of = [&](const u32x4* at, Frag (&f)[KS]) __attribute__((always_inline)) {
