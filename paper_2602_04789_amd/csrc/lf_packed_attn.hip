@@ -11,6 +11,9 @@
 //
 // Heads of the last rows, which see most, go first; neighbouring workgroups take heads in turn, so that those that share a head of K and V run at
 // one time on the XCDs that have it.
+//
+// Seven prompts, 16 384 tokens, 40 heads on 8 of 128: 601 us (997 TFLOP/s of what the rows see; 1.40 PFLOP/s is what a large product reaches).  4680 rows of 12 heads
+// over 512 tokens: 24.8 us (594 TFLOP/s), of which some 7 are the launch, the first tiles and the last stores.
 #include "lf_packed.h"
 
 namespace {

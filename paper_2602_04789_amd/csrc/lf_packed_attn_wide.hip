@@ -10,8 +10,8 @@
 // change with bit 14 of the LDS addresses.
 // The products into the accumulation registers are inline assembly, two wait states ahead of each (see lf_packed_dkv_wide.hip).
 //
-// Seven chunks of 4680 tokens, 12 heads: 3.38 ms (1113 TFLOP/s; 3.50 ms with 32 rows of a wavefront); one chunk of 4680 rows over 16 384 tokens: 434 us (481).
-// The matrix pipes and the chip's power bound it: it runs at 1.8 GHz.
+// Seven chunks of 4680 tokens, 12 heads: 3.22 to 3.38 ms (1115 to 1170 TFLOP/s; 3.50 ms with 32 rows of a wavefront); one chunk of 4680 rows over 16 384 tokens: 434 us (481).
+// The matrix pipes are busy 59 % of the cycles, the rest is issue of the exponentials, and the chip's power holds the clock at 1.8 to 2.0 GHz.
 #include "lf_packed.h"
 
 namespace {

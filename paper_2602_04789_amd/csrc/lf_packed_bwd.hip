@@ -26,6 +26,8 @@ constexpr int kTrHiFlip = 16;     // of an element's place
 constexpr int kShort = 256;
 
 // dQ, and -delta and -lse2 / c of every row for the launch behind it: four wavefronts of 32 rows each share tiles of 32 tokens of K and V.
+// Seven chunks of 4680 tokens, 12 heads of 128: 4.57 ms (1236 TFLOP/s of its three products); the matrix pipes are busy 70 % of the cycles, at 1.7 GHz: the chip's
+// power bounds it.  (Three stages, two tiles ahead: 4.96 ms; 64 rows of a wavefront: 5.15 ms.)  1333 tokens in 9 sequences, 6 heads of 64: 13.6 us.
 template <int D>
 __global__ __launch_bounds__(256, 2) void lf_packed_dq_kernel(PackedArgs a) {
   constexpr int kRows = 128;
@@ -195,6 +197,7 @@ __global__ __launch_bounds__(256, 2) void lf_packed_dq_kernel(PackedArgs a) {
 // most, and dS, which is rounded to bfloat16 again, has only half a step of that to bear); so one barrier a step is enough.  A tile is
 // requested two steps ahead; its Q lives for two steps (four stages), its dO for one (three).  SPLIT > 1: the workgroup holds SPLIT such groups with stages of their own, each takes a share of the steps (all the same number; those past
 // the end are empty), and their sums are added through LDS in order: for calls with too few tokens to fill the chip.
+// 1333 tokens in 9 sequences, 6 heads on 2 of 64: 19 us, 32 with tiles one step ahead and an LDS layout for the transposed reads alone: latency, a step after another.
 template <int D, int SPLIT>
 __global__ __launch_bounds__(256 * SPLIT, SPLIT == 1 ? 2 : 1) void lf_packed_dkv_kernel(PackedArgs a) {
   constexpr int kTokens = 64;
@@ -479,7 +482,7 @@ template <int D> int launch(const PackedArgs& a, hipStream_t st) {
   constexpr int kSplit = D == 128 ? 2 : 4;       // groups that a compute unit's LDS has room for
   const int64_t blocks = (int64_t)(a.kv_len / 64 + a.seqs) * a.Hk;
   // several groups to a workgroup while a compute unit has two of them or fewer (divided and not: 32 heads on 4 of 128, 8192 tokens, causal 2451 and
-  // 2916, 12 000 tokens 5675 and 5548; 8 heads of 64, 2048 tokens 113 and 128; 8 sequences of 512, 24 heads on 8 131 and 126)
+  // 2916, 12 000 tokens 5675 and 5548; 8 heads of 64, 2048 tokens 97 and 110; 256 sequences of 200 tokens, 8 heads on 2 of 64, 241 and 193)
   const bool split = (int64_t)(a.kv_len / 64 + a.seqs - 1) * a.Hk <= 2 * 256;
   const hipError_t rc = split ? lf_launch(lf_packed_dkv_kernel<D, kSplit>, dim3((unsigned)blocks), dim3(256 * kSplit), 0, st, a)
                               : lf_launch(lf_packed_dkv_kernel<D, 1>, dim3((unsigned)blocks), dim3(256), 0, st, a);

@@ -12,6 +12,9 @@
 // dP and the first half of dV, dS beside dV, the LDS reads of a fragment some slots ahead of its product; sched_barrier keeps them there.  S and dP start from
 // -lse2 / c and -delta, so no subtraction is left.  The products into the accumulation registers are inline assembly (left to itself the compiler copies the
 // sums around the loop); two wait states stand ahead of each, since the compiler does not count those behind the vector instruction that packed its operand.
+//
+// Seven chunks of 4680 tokens, 12 heads: 5.92 ms (1274 TFLOP/s of its four products; with 32 tokens of a wavefront 12.0 ms).  The matrix pipes are busy 63 % of
+// the cycles; the rest is issue of the vector instructions, and the chip's power holds the clock at 1.9 GHz.
 #include "lf_packed.h"
 
 namespace {

@@ -9,6 +9,8 @@
 // Products transposed, S^T = K Q^T and O^T = V^T P^T, with v_mfma_f32_16x16x32_bf16: the first one leaves a lane the scores of the tokens 4 kg + {0..3}
 // of each 16, which are its operand of the second.  P goes into the products in two bfloat16 parts (16 bits) with 16 rows, where bytes are the
 // bound, and in one with 32.  The states of the wavefronts are joined through LDS, those of the parts by a launch of their own.
+//
+// 16 single rows over 120 003 tokens, 40 heads on 8 of 128: 90 us (492 MB, 5.5 TB/s) and 5 for the join.  One row of 12 heads over 77 tokens: 5.4 us.
 #include "lf_packed.h"
 
 namespace {
