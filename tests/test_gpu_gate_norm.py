@@ -153,6 +153,13 @@ def test_what_may_be_left_out(gpu, off):
         _run(gpu, 21, 328, group_len=8, layer=layer, post=off in ("gate", "shift"), seed=4, **{off: False})
 
 
+@pytest.mark.parametrize("off", ["gate", "weight", "scale", "block"])
+@pytest.mark.parametrize("kw", [dict(group_len=23), dict(starts=[0, 23]), dict(starts=[4, 4])])
+def test_one_group(gpu, off, kw):
+    """Its sums are those of the weights too."""
+    _run(gpu, 23, 200, post=off != "block", seed=5, **{off: False}, **kw)
+
+
 def test_nothing_but_the_norm(gpu):
     _run(gpu, 9, 128, group_len=9, block=False, weight=False, scale=False, shift=False)
 
