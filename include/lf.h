@@ -590,13 +590,13 @@ int lf_gate_norm_bwd(const void* Xout, const void* B, const float* gate, const f
  *   q_start, kv_start   device, int32 [seqs + 1], ascending, 0 .. q_len and 0 .. kv_len.  Not checked: nothing outside the tensors is touched
  *              for any values, but results are right for ascending ones only.
  *   lse2       device, float32 [heads][q_len], contiguous; the forward call may be given NULL.
- *   softmax_scale  0 selects 1 / sqrt(head_dim).
+ *   softmax_scale  0 selects 1 / sqrt(head_dim); else 1e-30 .. 1e20, and logits q . k softmax_scale within 5e29 of 0.
  *   workspace  device scratch of >= lf_packed_attn_workspace_bytes() (lf_packed_attn_bwd_workspace_bytes()), 256-byte aligned, may be NULL where that is 0.
  *              Calls that may overlap must not share it.
  * Inputs must be finite.  Outputs overlap nothing else.
  * Errors: LF_ERR_NULL; LF_ERR_SHAPE (head_dim not 64 or 128; kv_heads not in 1 .. 4 096 or heads no multiple of it in 1 .. 256 times it; seqs not in
  *   1 .. 2^20; q_len and kv_len not in 0 .. 2^30; causal not in 0 .. 2^30; a token stride not in head_dim .. 2^20, a head stride not in 0 .. 2^44; heads of an
- *   output that share an element; a call, forward or backward, of 2^24 workgroups or more; softmax_scale negative or not finite); LF_ERR_DTYPE; LF_ERR_ALIGN; LF_ERR_WORKSPACE; LF_ERR_HIP.
+ *   output that share an element; a call, forward or backward, of 2^24 workgroups or more; softmax_scale not 0 and not in 1e-30 .. 1e20); LF_ERR_DTYPE; LF_ERR_ALIGN; LF_ERR_WORKSPACE; LF_ERR_HIP.
  * q_len = 0 or kv_len = 0: rows are zeros, gradients of tokens are zeros.
  */
 typedef struct {

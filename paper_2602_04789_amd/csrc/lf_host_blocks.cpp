@@ -90,7 +90,8 @@ int check_packed(const lf_packed_shape* s) {
                       check_stride(s->v_stride_tok, s->v_stride_head, s->head_dim), check_stride(s->o_stride_tok, s->o_stride_head, s->head_dim)};
   return first_error(all, 4);
 }
-bool scale_ok(float s) { return s >= 0.0f && !isinf(s); }
+// The gradients divide the log-sum-exp by it, and logits are taken to lie above -1e30.
+bool scale_ok(float s) { return s == 0.0f || (s >= 1e-30f && s <= 1e20f); }
 float scale_or_default(float s, int d) { return s > 0.0f ? s : 1.0f / sqrtf((float)d); }
 
 // ---- gradient clipping ----

@@ -96,8 +96,9 @@ def test_packed_attention_refuses_bad_arguments(lib):
     assert lib.lf_packed_attn(FAKE, FAKE, FAKE, None, FAKE, FAKE, 0.0, FAKE, None, None, 0, None) == -1
     for kw, code in BAD_PACKED + [(dict(o_stride_head=64), -2)]:
         assert call(s=_packed(**kw)) == code, kw
-    for scale in (-1.0, float("nan"), float("inf")):
+    for scale in (-1.0, float("nan"), float("inf"), 1e-40, 0.99e-30, 1.01e20, 3e38):
         assert call(scale=scale) == -2
+    assert all(call(s=_packed(**few), scale=scale, n=need - 1) == -6 for scale in (0.0, 1e-30, 1e20))
     assert need > 0 and call(s=_packed(**few), n=need - 1) == -6 and call(s=_packed(**few), ws=None, n=need) == -6 and call(s=_packed(**few), ws=FAKE + 16, n=need) == -5
     for k in ("Q", "K", "V", "O"):
         assert call(**{k: FAKE + 8}) == -5
@@ -115,7 +116,7 @@ def test_packed_backward_refuses_bad_arguments(lib):
         assert call(**{k: None}) == -1, k
     for kw, code in BAD_PACKED + [(dict(q_stride_head=64), -2), (dict(k_stride_head=0), -2), (dict(v_stride_head=128), -2)]:
         assert call(s=_packed(**kw), n=1 << 60) == code, kw
-    assert call(scale=-1.0) == -2 and call(ws=None) == call(n=need - 1) == -6
+    assert call(scale=-1.0) == call(scale=1e-31) == call(scale=1e21) == -2 and call(scale=1e-30, n=need - 1) == -6 and call(ws=None) == call(n=need - 1) == -6
     for k in ("Q", "K", "V", "O", "dO", "dQ", "dK", "dV"):
         assert call(**{k: FAKE + 8}) == -5, k
     assert call(ws=FAKE + 16) == call(l=FAKE + 2) == call(a=FAKE + 1) == -5

@@ -172,6 +172,12 @@ def test_many_rows_of_many_tokens(gpu, H, Hk, q, kv, causal, layout, pad):
     _run(gpu, H, Hk, 128, q, kv, causal, seed=8, layout=layout, pad=pad, train=False)
 
 
+@pytest.mark.parametrize("H,Hk,d,q,kv,causal", [(2, 1, 64, [0, 3, 150], [0, 9, 200], 1), (2, 2, 128, [0, 200], [0, 700], 0), (14, 14, 128, [0, 130], [0, 2051], 0)])
+def test_the_smallest_scale(gpu, H, Hk, d, q, kv, causal):
+    """All logits are 0 but for 1e-30 of something: means, in every gradient kernel."""
+    _run(gpu, H, Hk, d, q, kv, causal, seed=13, softmax_scale=1.0000001e-30)
+
+
 def test_many_rows_of_rising_logits(gpu):
     """Keys that grow along 4200 tokens, then the same ones backwards: the reference moves at every tile, or only at the first."""
     torch, lf = gpu
