@@ -160,6 +160,26 @@ def test_one_group(gpu, off, kw):
     _run(gpu, 23, 200, post=off != "block", seed=5, **{off: False}, **kw)
 
 
+@pytest.mark.parametrize("C", [72, 1536, 2048, 8200])
+@pytest.mark.parametrize("starts", [[2, 9, 30], [3, 3, 31]])
+def test_nan_beside_the_groups_stays_there(gpu, C, starts):
+    torch, lf = gpu
+    L, G = 37, len(starts) - 1
+    t = _inputs(torch, L, C, G, False, 6, 0)
+    st = torch.tensor(starts, dtype=torch.int32, device="cuda")
+    how = dict(B=t["B"], gate=t["gate"], post_weight=t["post"], weight=t["weight"], scale=t["scale"], starts=st)
+    results = []
+    for beside in (0.0, float("nan")):
+        for k in ("X", "B", "dY", "dXout"):
+            t[k][:starts[0]] = beside
+            t[k][starts[-1]:] = beside
+        X1, Y = lf.lf_gate_norm(t["X"], shift=t["shift"], Xout=torch.full_like(t["X"], beside), **how)
+        dX, dB, *tables = lf.lf_gate_norm_bwd(X1, t["dY"], dXout=t["dXout"], **how)
+        results.append([x[starts[0]:starts[-1]] for x in (X1, Y, dX, dB)] + tables)
+    for a, b in zip(*results):
+        assert torch.equal(a, b) and not torch.isnan(a).any()
+
+
 def test_nothing_but_the_norm(gpu):
     _run(gpu, 9, 128, group_len=9, block=False, weight=False, scale=False, shift=False)
 

@@ -356,6 +356,30 @@ def test_starts_of_any_values_touch_nothing_outside(gpu):
             assert (b[:, :3] == 7.0).all()
 
 
+@pytest.mark.parametrize("H,Hk,d,q,kv,causal", [(4, 2, 64, [5, 38, 201], [3, 70, 180], 1), (4, 2, 128, [5, 38, 201], [3, 70, 180], 0), (8, 2, 128, [2, 3, 5], [70, 800, 3001], 1),
+                                                (8, 2, 64, [2, 22, 49], [70, 800, 3001], 0), (14, 14, 128, [7, 70, 141], [5, 1000, 2060], 0), (30, 30, 128, [9, 1100], [2, 8300], 1)])
+def test_nan_beside_the_sequences_stays_there(gpu, H, Hk, d, q, kv, causal):
+    """Rows and tokens of no sequence hold NaN, in every kernel."""
+    torch, lf = gpu
+    L, T = q[-1] + 9, kv[-1] + 77
+    print(f"nan beside H={H} Hk={Hk} d={d} q={q} kv={kv} causal={causal}", flush=True)
+    g = torch.Generator(device="cuda").manual_seed(0)
+    make = lambda *s: torch.randn(s, generator=g, device="cuda").to(torch.bfloat16)
+    Q, K, V, dO = make(H, L, d), make(Hk, T, d), make(Hk, T, d), make(H, L, d)
+    qs, ks = (torch.tensor(s, dtype=torch.int32, device="cuda") for s in (q, kv))
+    results = []
+    for beside in (0.0, float("nan")):
+        for t, s in ((Q, q), (dO, q), (K, kv), (V, kv)):
+            t[:, :s[0]] = beside
+            t[:, s[-1]:] = beside
+        O, lse2 = torch.full_like(Q, beside), torch.full((H, L), beside, device="cuda")
+        lf.lf_packed_attn_fwd(Q, K, V, qs, ks, causal=causal, O=O, lse2=lse2)
+        grads = lf.lf_packed_attn_bwd(Q, K, V, O, dO, lse2, qs, ks, causal=causal)
+        results.append([O[:, q[0]:q[-1]], lse2[:, q[0]:q[-1]], grads[0][:, q[0]:q[-1]]] + [x[:, kv[0]:kv[-1]] for x in grads[1:]])
+    for a, b in zip(*results):
+        assert torch.equal(a, b) and not torch.isnan(a).any()
+
+
 def test_results_are_the_same_again_and_on_another_stream(gpu):
     torch, lf = gpu
     g = torch.Generator().manual_seed(4)
