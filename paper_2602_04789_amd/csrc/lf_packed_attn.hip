@@ -12,8 +12,9 @@
 // Heads of the last rows, which see most, go first; neighbouring workgroups take heads in turn, so that those that share a head of K and V run at
 // one time on the XCDs that have it.
 //
-// Seven prompts, 16 384 tokens, 40 heads on 8 of 128: 601 us (997 TFLOP/s of what the rows see; 1.40 PFLOP/s is what a large product reaches).  4680 rows of 12 heads
-// over 512 tokens: 24.8 us (594 TFLOP/s), of which some 7 are the launch, the first tiles and the last stores.
+// Seven prompts, 16 384 tokens, 40 heads on 8 of 128: 580 us (1033 TFLOP/s of what the rows see; 1.40 PFLOP/s is what a large product reaches; 601 us with the products and
+// the exponentials of a tile one after the other).  Seven chunks of 4680 tokens, 12 heads: 3.28 ms (1150 TFLOP/s).  4680 rows of 12 heads over 512 tokens: 23.1 us
+// (637 TFLOP/s), of which some 7 are the launch, the first tiles and the last stores.
 #include "lf_packed.h"
 
 namespace {
@@ -25,13 +26,16 @@ template <int CH> __device__ __forceinline__ int v_swz(int row, int ch) {
   return CH == 16 ? ch ^ ((row & 3) << 2) : ch ^ (((row >> 1) & 1) << 2);
 }
 
+typedef __attribute__((address_space(3))) const u32x4* LdsRow;
+typedef __attribute__((address_space(3))) bf16x4* LdsQuad;
+
 template <int D>
 __global__ __launch_bounds__(256, 2) void lf_packed_attn_kernel(PackedArgs a) {
   constexpr int CH = D / 8, KS = D / 16, MB = D / 32;
   constexpr int TILE = kTok * CH;           // 16-byte chunks of K or V of a tile
   constexpr int LPW = TILE / 64 / 4;        // load instructions of a wavefront for K or V of a tile
   constexpr int RPI = 64 / CH;              // rows of a load instruction
-  __shared__ u32x4 stage[2][2 * TILE];      // K | V
+  __shared__ __attribute__((aligned(64 * TILE))) u32x4 stage[2][2 * TILE];      // K | V: the stages differ in one bit of an address
 
   int x = blockIdx.x;
   const int hk = x % a.Hk;
@@ -87,88 +91,130 @@ __global__ __launch_bounds__(256, 2) void lf_packed_attn_kernel(PackedArgs a) {
     fetch<LPW>(rows_rsrc(Kh, (int64_t)s.k0 + t, n, k_row), lds_addr(to + LPW * 64 * wave), koff);
     fetch<LPW>(rows_rsrc(Vh, (int64_t)s.k0 + t, n, v_row), lds_addr(to + TILE + LPW * 64 * wave), voff);
   };
-  int kaddr[KS], vbase[MB];
+  // addresses in the present stage
+  const uint32_t base = __builtin_amdgcn_readfirstlane(lds_addr(&stage[0][0]));
+  uint32_t kaddr[KS], vaddr[MB];
 #pragma unroll
-  for (int k = 0; k < KS; ++k) kaddr[k] = ln * CH + row_swz<CH>(ln, 2 * k + kg);
+  for (int k = 0; k < KS; ++k) kaddr[k] = base + 16u * (ln * CH + row_swz<CH>(ln, 2 * k + kg));
   {
     const int i16 = lane & 15, tr_row = 4 * kg + (i16 >> 2), tr_col = 16 * ((lane >> 4) & 1) + 4 * (i16 & 3);
 #pragma unroll
     for (int mb = 0; mb < MB; ++mb) {
       const int col = 32 * mb + tr_col;
-      vbase[mb] = (tr_row * CH + v_swz<CH>(tr_row, col >> 3)) * 8 + (col & 7);
+      vaddr[mb] = base + 16u * TILE + 2u * ((tr_row * CH + v_swz<CH>(tr_row, col >> 3)) * 8 + (col & 7));
     }
   }
+  auto other_stage = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int k = 0; k < KS; ++k) kaddr[k] ^= 32u * TILE;
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb) vaddr[mb] ^= 32u * TILE;
+  };
 
   f32x16 oacc[MB];
 #pragma unroll
   for (int mb = 0; mb < MB; ++mb) oacc[mb] = zero16();
   constexpr float kSumMax = 1.0e30f;
   float m_run = -1.0e30f, l_run = 0.0f;
-  auto row_max = [](const f32x16& x) __attribute__((always_inline)) {
-    float m = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
-#pragma unroll
-    for (int i = 4; i < 16; i += 2) m = fmaxf(m, fmaxf(x[i], x[i + 1]));
-    return m;
-  };
   const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
 
-  // One tile of tokens [t, t + 64) of the sequence.
-  auto work = [&](int t, const u32x4* at) __attribute__((always_inline)) {
-    f32x16 sc[2];
-#pragma unroll
-    for (int hf = 0; hf < 2; ++hf) {
-      Frag kf[KS];
-#pragma unroll
-      for (int k = 0; k < KS; ++k) kf[k].u = at[kaddr[k] + 32 * hf * CH];
-      sc[hf] = zero16();
-#pragma unroll
-      for (int k = 0; k < KS; ++k) sc[hf] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[k].v, qf[k].v, sc[hf], 0, 0, 0);
-    }
-    if (t + kTok > lim_first) {      // accumulator i: token 8 (i / 4) + 4 kg + i mod 4 of the half tile
-#pragma unroll
-      for (int hf = 0; hf < 2; ++hf)
+  // One tile of tokens [t, t + 64) of the sequence, in halves: S of the first, S of the second beside the exponentials of the first, O of the first beside those
+  // of the second, O of the second.  A slot holds one product, the LDS reads of a fragment of the next block and a share of the exponentials, which go
+  // through their stages (scale, exp2, pack and sum) a beat each; sched_barrier keeps the slots as written.
+  auto work = [&](int t) __attribute__((always_inline)) {
+    static_assert(KS == 2 * MB, "a half tile has as many products of S as of O");
+    constexpr int kBeats = 16 / KS;           // of a slot
+    Frag k0[KS], k1[KS];
+    bf16x8 v0[KS], v1[KS], p0[2], p1[2];
+    f32x16 s0 = zero16(), s1 = zero16();
+    auto v_frag = [&](int hf, int n) __attribute__((always_inline)) {
+      const int u = 2 * hf + n / MB, mb = n % MB;
+      const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LdsQuad)(uintptr_t)(vaddr[mb] + 16u * CH * (16 * u)));
+      const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LdsQuad)(uintptr_t)(vaddr[mb] + 16u * CH * (16 * u + 8)));
+      return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    };
+    auto mask = [&](int hf, f32x16& sc) __attribute__((always_inline)) {      // accumulator i: token 8 (i / 4) + 4 kg + i mod 4 of the half tile
+      if (t + 32 * hf + 32 > lim_first) {
+        const int past = lim - t - 32 * hf - 4 * kg;
 #pragma unroll
         for (int i = 0; i < 16; ++i)
-          if (t + 32 * hf + 8 * (i >> 2) + 4 * kg + (i & 3) >= lim) sc[hf][i] = -INFINITY;
-    }
-    bf16x8 pf[4];
-    float l_new;
-    auto softmax = [&](float l0) __attribute__((always_inline)) {
-      l_new = l0;
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) pf[u][e] = (__bf16)__builtin_amdgcn_exp2f(fmaf(sc[u >> 1][8 * (u & 1) + e], a.c, -m_run));
-#pragma unroll
-        for (int e = 0; e < 8; e += 2) {
-          const bf16x2 pr = {pf[u][e], pf[u][e + 1]};
-          l_new = __builtin_amdgcn_fdot2_f32_bf16(pr, ones, l_new, false);
-        }
+          if (8 * (i >> 2) + (i & 3) >= past) sc[i] = -INFINITY;
       }
     };
-    softmax(l_run);
-    if (__ballot(l_new > kSumMax) != 0ull) {
-      float top = fmaxf(row_max(sc[0]), row_max(sc[1]));
-      const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
-      top = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * a.c;
-      const float m_new = fmaxf(m_run, top), alpha = __builtin_amdgcn_exp2f(m_run - m_new);
-      m_run = m_new;
-#pragma unroll
-      for (int mb = 0; mb < MB; ++mb)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) oacc[mb][i] *= alpha;
-      softmax(l_run * alpha);
-    }
-    l_run = l_new;
-    const uint16_t* v16 = reinterpret_cast<const uint16_t*>(at + TILE);
-#pragma unroll
-    for (int u = 0; u < 4; ++u)
-#pragma unroll
-      for (int mb = 0; mb < MB; ++mb) {
-        const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(LDS_PTR(bf16x4, v16 + vbase[mb] + 16 * u * CH * 8));
-        const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(LDS_PTR(bf16x4, v16 + vbase[mb] + (16 * u + 8) * CH * 8));
-        oacc[mb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7), pf[u], oacc[mb], 0, 0, 0);
+    float x[2], y[2], l_new;
+    auto beat = [&](int n, const f32x16& sc, bf16x8 (&p)[2]) __attribute__((always_inline)) {      // 18 of them
+      if (n >= 2 && (n & 1)) {
+        const int v = n - 2;
+        const bf16x2 pr = {(__bf16)y[0], (__bf16)y[1]};
+        p[v >> 3][(v & 7) - 1] = pr[0];
+        p[v >> 3][v & 7] = pr[1];
+        l_new = __builtin_amdgcn_fdot2_f32_bf16(pr, ones, l_new, false);
       }
+      if (n >= 1 && n < 17) y[(n - 1) & 1] = __builtin_amdgcn_exp2f(x[(n - 1) & 1]);
+      if (n < 16) x[n & 1] = fmaf(sc[n], a.c, -m_run);
+    };
+    // behind the exponentials of a half: the reference moves where the row's sum is about to leave the range
+    auto check = [&](const f32x16& sc, bf16x8 (&p)[2]) __attribute__((always_inline)) {
+      if (__ballot(l_new > kSumMax) != 0ull) {
+        float top = fmaxf(sc[0], sc[1]);
+#pragma unroll
+        for (int i = 2; i < 16; i += 2) top = fmaxf(top, fmaxf(sc[i], sc[i + 1]));
+        const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+        top = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * a.c;
+        const float m_new = fmaxf(m_run, top), alpha = __builtin_amdgcn_exp2f(m_run - m_new);
+        m_run = m_new;
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) oacc[mb][i] *= alpha;
+        l_new = l_run * alpha;
+#pragma unroll
+        for (int n = 0; n < 18; ++n) beat(n, sc, p);
+      }
+      l_run = l_new;
+    };
+#pragma unroll
+    for (int n = 0; n < KS; ++n) k0[n].u = *(LdsRow)(uintptr_t)kaddr[n];
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int n = 0; n < KS; ++n) {
+      s0 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k0[n].v, qf[n].v, s0, 0, 0, 0);
+      k1[n].u = *(LdsRow)(uintptr_t)(kaddr[n] + 512u * CH);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    mask(0, s0);
+    l_new = l_run;
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int n = 0; n < KS; ++n) {
+      s1 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k1[n].v, qf[n].v, s1, 0, 0, 0);
+      v0[n] = v_frag(0, n);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int i = 0; i < kBeats; ++i)
+        if (n > 0) beat(kBeats * (n - 1) + i, s0, p0);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+    for (int i = 16 - kBeats; i < 18; ++i) beat(i, s0, p0);
+    check(s0, p0);
+    mask(1, s1);
+    l_new = l_run;
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int n = 0; n < KS; ++n) {
+      oacc[n % MB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v0[n], p0[n / MB], oacc[n % MB], 0, 0, 0);
+      v1[n] = v_frag(1, n);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int i = 0; i < kBeats; ++i) beat(kBeats * n + i, s1, p1);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    beat(16, s1, p1);
+    beat(17, s1, p1);
+    check(s1, p1);
+#pragma unroll
+    for (int n = 0; n < KS; ++n) oacc[n % MB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v1[n], p1[n / MB], oacc[n % MB], 0, 0, 0);
   };
   if (t0 < t1) request(t0, stage[0]);
   int cur = 0;
@@ -176,7 +222,8 @@ __global__ __launch_bounds__(256, 2) void lf_packed_attn_kernel(PackedArgs a) {
     __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));     // this wavefront's share of the tile
     lds_barrier();                                // everyone's, and nobody reads the other stage any more
     if (t + kTok < t1) request(t + kTok, stage[cur ^ 1]);
-    if (t < lim_last) work(t, stage[cur]);
+    if (t < lim_last) work(t);
+    other_stage();
   }
 
   const float l = l_run + __shfl_xor(l_run, 32);
@@ -300,11 +347,10 @@ int lf_launch_packed_attn(const lf_packed_call* c, void* stream) {
   const PackedArgs a = lf_packed_args(c);
   const int d = c->s->head_dim;
   hipStream_t st = (hipStream_t)stream;
-  // 64 rows of a wavefront where a sequence's rows see 4096 tokens or more in the mean (us, 32 and 64 rows): 40 heads, 4680 rows of 4680 tokens 442 and 421,
-  // of 18 720 tokens 1785 and 1652; 12 heads, 4096 tokens 90 and 90, 512 tokens 16 and 24 (its start and end take 6 us more); causal, 40 heads of 4680 tokens
-  // 229 and 246, of 8192 tokens 663 and 656, of 16 384 tokens 2617 and 2522.
-  const int64_t seen = c->s->kv_len / (c->s->causal ? 2 : 1);
-  if (d == 128 && a.parts == 1 && c->s->q_len >= 512 * (int64_t)c->s->seqs && seen >= 4096 * (int64_t)c->s->seqs) return lf_launch_packed_attn_wide(a, st);
+  // 64 rows of a wavefront where rows see all of 8192 tokens or more in the mean (us, 32 and 64 rows: 12 heads, 4096 rows of 4096 tokens 110 and 112; 4680 rows of 8192
+  // tokens 223 and 216, of 16 384 tokens 435 and 422; 40 heads of 18 720 tokens 1677 and 1613; causal, 40 heads of 8192 tokens 620 and 650, of 16 384 tokens 2449 and 2460).
+  if (d == 128 && a.parts == 1 && a.unit == 0 && c->s->q_len >= 512 * (int64_t)c->s->seqs && c->s->kv_len >= 8192 * (int64_t)c->s->seqs)
+    return lf_launch_packed_attn_wide(a, st);
   const dim3 grid((unsigned)((int64_t)a.slots * a.H * a.parts));
   const hipError_t rc = d == 128 ? lf_launch(lf_packed_attn_kernel<128>, grid, dim3(256), 0, st, a)
                                  : lf_launch(lf_packed_attn_kernel<64>, grid, dim3(256), 0, st, a);

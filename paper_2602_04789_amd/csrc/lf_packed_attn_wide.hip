@@ -1,4 +1,4 @@
-// Attention over packed sequences at head dimension 128, for calls with enough rows: one wavefront per SIMD, 64 rows of a wavefront.
+// Attention over packed sequences at head dimension 128, for calls of many rows that see many tokens: one wavefront per SIMD, 64 rows of a wavefront.
 //
 // As lf_packed_attn.hip, with 256 rows of a workgroup: a fragment of K or V that a wavefront reads from LDS feeds two products, one for each half of its
 // rows, so LDS delivers half as much for a product.  The rows of Q and the sums of O are in the accumulation half of the register file.
@@ -10,7 +10,7 @@
 // change with bit 14 of the LDS addresses.
 // The products into the accumulation registers are inline assembly, two wait states ahead of each (see lf_packed_dkv_wide.hip).
 //
-// Seven chunks of 4680 tokens, 12 heads: 3.22 to 3.38 ms (1115 to 1170 TFLOP/s; 3.50 ms with 32 rows of a wavefront); one chunk of 4680 rows over 16 384 tokens: 434 us (481).
+// 4680 rows of 12 heads over 16 384 tokens: 422 us (1117 TFLOP/s; 435 with 32 rows of a wavefront); seven chunks of 4680 tokens 3.26 ms (3.28).
 // The matrix pipes are busy 59 % of the cycles, the rest is issue of the exponentials, and the chip's power holds the clock at 1.8 to 2.0 GHz.
 #include "lf_packed.h"
 

@@ -164,11 +164,11 @@ def test_many_tokens_by_chunks(gpu):
 
 
 @pytest.mark.parametrize("H,Hk,q,kv,causal,layout,pad", [
-    (24, 8, [0, 700, 1400], [0, 3001, 8300], 0, "heads", 0), (32, 32, [0, 1100], [0, 8193], 1, "tokens", 8),
-    (27, 9, [3, 903, 1290], [5, 9000, 16500], 300, "heads", 24), (16, 4, [0, 1, 1, 700, 2063], [0, 4000, 4100, 12000, 16500], 0, "tokens", 0),
+    (24, 8, [0, 700, 1400], [0, 3001, 16500], 0, "heads", 0), (24, 8, [2, 702, 1403], [3, 3001, 16500], 0, "tokens", 8), (12, 12, [0, 700, 2100], [0, 0, 16500], 0, "heads", 16), (32, 32, [0, 1100], [0, 8193], 1, "tokens", 8),
+    (27, 9, [3, 903, 1290], [5, 9000, 16500], 300, "heads", 24), (16, 4, [0, 1, 1, 700, 2063], [0, 4000, 4100, 12000, 32900], 0, "tokens", 0),
     (12, 12, [0, 2100, 3074], [0, 1500, 20000], 1, "heads", 0)])
 def test_many_rows_of_many_tokens(gpu, H, Hk, q, kv, causal, layout, pad):
-    """The kernel of 64 rows a wavefront: 4096 tokens or more that a row sees in the mean.  In the last case 600 rows see nothing."""
+    """The kernel of 64 rows a wavefront (8192 tokens or more in the mean, all seen), and causal calls of such sizes.  In some cases there are rows that see nothing."""
     _run(gpu, H, Hk, 128, q, kv, causal, seed=8, layout=layout, pad=pad, train=False)
 
 
@@ -178,17 +178,18 @@ def test_the_smallest_scale(gpu, H, Hk, d, q, kv, causal):
     _run(gpu, H, Hk, d, q, kv, causal, seed=13, softmax_scale=1.0000001e-30)
 
 
-def test_many_rows_of_rising_logits(gpu):
-    """Keys that grow along 4200 tokens, then the same ones backwards: the reference moves at every tile, or only at the first."""
+@pytest.mark.parametrize("n", [4200, 8200])
+def test_many_rows_of_rising_logits(gpu, n):
+    """Keys that grow along the tokens, then the same ones backwards: the reference moves at every tile, or only at the first."""
     torch, lf = gpu
-    H, rows, n, d = 24, 1401, 4200, 128
+    H, rows, d = 24, 1401, 128
     g = torch.Generator().manual_seed(3)
     u = torch.nn.functional.normalize(torch.randn(d, generator=g), dim=0)
     Q = (11.3 * u).repeat(1, rows, 1).to(torch.bfloat16)
     V = torch.randn((1, n, d), generator=g).to(torch.bfloat16)
     qs, ks = torch.tensor([0, rows], dtype=torch.int32, device="cuda"), torch.tensor([0, n], dtype=torch.int32, device="cuda")
     for order in (torch.arange(n), n - torch.arange(n)):
-        K = (order[:, None] * u * 0.19).to(torch.bfloat16)[None]
+        K = (order[:, None] * u * (0.19 * 4200 / n)).to(torch.bfloat16)[None]
         O = lf.lf_packed_attn(Q.cuda().expand(H, rows, d).contiguous(), K.cuda().expand(H, n, d).contiguous(), V.cuda().expand(H, n, d).contiguous(), qs, ks)
         assert torch.equal(O, O[:1].expand_as(O))
         ref, _, size = R.packed_attention(_np(Q[:, :1]), _np(K), _np(V), [0, 1], [0, n], 0, d ** -0.5)
@@ -357,7 +358,7 @@ def test_starts_of_any_values_touch_nothing_outside(gpu):
 
 
 @pytest.mark.parametrize("H,Hk,d,q,kv,causal", [(4, 2, 64, [5, 38, 201], [3, 70, 180], 1), (4, 2, 128, [5, 38, 201], [3, 70, 180], 0), (8, 2, 128, [2, 3, 5], [70, 800, 3001], 1),
-                                                (8, 2, 64, [2, 22, 49], [70, 800, 3001], 0), (14, 14, 128, [7, 70, 141], [5, 1000, 2060], 0), (30, 30, 128, [9, 1100], [2, 8300], 1)])
+                                                (8, 2, 64, [2, 22, 49], [70, 800, 3001], 0), (14, 14, 128, [7, 70, 141], [5, 1000, 2060], 0), (30, 30, 128, [9, 1100], [2, 8300], 1), (30, 30, 128, [9, 1100], [2, 8300], 0)])
 def test_nan_beside_the_sequences_stays_there(gpu, H, Hk, d, q, kv, causal):
     """Rows and tokens of no sequence hold NaN, in every kernel."""
     torch, lf = gpu
