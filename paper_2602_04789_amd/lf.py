@@ -1113,32 +1113,30 @@ def lf_grad_clip(grads, max_norm: float, out=None, eps: float = 1e-6, norm=None,
     kinds = _stream_dtypes or _dtypes()
     grads = list(grads)
     at, st = _here(stream)
+    to = None if out is None else list(out)
+    tensors = grads if to is None else grads + to
+    T = torch.Tensor
+    if any(x != at for x in map(T.get_device, tensors)):
+        raise ValueError("all tensors must live on the current device")
+    sizes = list(map(T.numel, grads))
     # the C structures as rows of four 64-bit numbers: address, address or 0, elements, the two types (a third of the time that ctypes takes for them)
-    rows, total = array.array("q"), 0
+    rows = array.array("q", bytes(32 * len(grads)))
     try:
-        if out is None:
-            for x in grads:
-                if x.get_device() != at:
-                    raise ValueError("all tensors must live on the current device")
-                if not x.is_contiguous() and not _dense(x):
-                    raise ValueError("gradients must be contiguous (in place: without holes)")
-                n = x.numel()
-                rows.extend((x.data_ptr(), 0, n, kinds[x.dtype]))
-                total += n
+        types = [kinds[x.dtype] for x in grads]
+        if to is None:
+            if not all(x.is_contiguous() or _dense(x) for x in grads):
+                raise ValueError("gradients must be contiguous (in place: without holes)")
         else:
-            to = list(out)
             if len(to) != len(grads):
                 raise ValueError("out must have a tensor for each gradient")
-            for x, y in zip(grads, to):
-                if x.get_device() != at or y.get_device() != at:
-                    raise ValueError("all tensors must live on the current device")
-                n = x.numel()
-                if y.numel() != n or not x.is_contiguous() or not y.is_contiguous():
-                    raise ValueError("gradients and out must be contiguous tensors of the same sizes")
-                rows.extend((x.data_ptr(), y.data_ptr(), n, kinds[x.dtype] | kinds[y.dtype] << 32))
-                total += n
+            if list(map(T.numel, to)) != sizes or not all(map(T.is_contiguous, tensors)):
+                raise ValueError("gradients and out must be contiguous tensors of the same sizes")
+            types = [k | kinds[y.dtype] << 32 for k, y in zip(types, to)]
+            rows[1::4] = array.array("q", map(T.data_ptr, to))
     except KeyError:
         raise ValueError("gradients and out must be bfloat16 or float32") from None
+    rows[0::4], rows[2::4], rows[3::4] = (array.array("q", x) for x in (map(T.data_ptr, grads), sizes, types))
+    total = sum(sizes)
     if norm is None:
         norm = _new(stream, torch.empty, (1,), dtype=torch.float32, device=_device(at))
     if norm.dtype is not torch.float32 or norm.numel() != 1 or norm.get_device() != at:
