@@ -347,10 +347,11 @@ int lf_launch_packed_attn(const lf_packed_call* c, void* stream) {
   const PackedArgs a = lf_packed_args(c);
   const int d = c->s->head_dim;
   hipStream_t st = (hipStream_t)stream;
-  // 64 rows of a wavefront where rows see all of 8192 tokens or more in the mean (us, 32 and 64 rows: 12 heads, 4096 rows of 4096 tokens 110 and 112; 4680 rows of 8192
-  // tokens 223 and 216, of 16 384 tokens 435 and 422; 40 heads of 18 720 tokens 1677 and 1613; causal, 40 heads of 8192 tokens 620 and 650, of 16 384 tokens 2449 and 2460).
-  if (d == 128 && a.parts == 1 && a.unit == 0 && c->s->q_len >= 512 * (int64_t)c->s->seqs && c->s->kv_len >= 8192 * (int64_t)c->s->seqs)
-    return lf_launch_packed_attn_wide(a, st);
+  // 64 rows of a wavefront where rows see 8192 tokens or more in the mean, unless each sees another one more (us, 32 and 64 rows: 12 heads, 4096 rows of 4096 tokens 110 and
+  // 112; 4680 rows of 8192 tokens 223 and 216, of 16 384 tokens 435 and 422; 40 heads of 18 720 tokens 1677 and 1613; by chunks of 4680, 12 heads of 32 760 tokens 3277
+  // and 3257, with the gradients, which the chip's power slows, 14 570 and 14 250; causal, 40 heads of 8192 tokens 620 and 650, of 16 384 tokens 2449 and 2460).
+  const int64_t seen = c->s->kv_len / (a.unit ? 2 : 1);
+  if (d == 128 && a.parts == 1 && a.unit != 1 && c->s->q_len >= 512 * (int64_t)c->s->seqs && seen >= 8192 * (int64_t)c->s->seqs) return lf_launch_packed_attn_wide(a, st);
   const dim3 grid((unsigned)((int64_t)a.slots * a.H * a.parts));
   const hipError_t rc = d == 128 ? lf_launch(lf_packed_attn_kernel<128>, grid, dim3(256), 0, st, a)
                                  : lf_launch(lf_packed_attn_kernel<64>, grid, dim3(256), 0, st, a);
