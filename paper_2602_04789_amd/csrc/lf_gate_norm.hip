@@ -12,8 +12,10 @@
 // from row to row, and the next row is requested before the present one is summed.  Sums over a row go across the lanes of a wavefront and,
 // where a row takes several, through LDS.  Sums over rows stay in registers over a slot (rows of one group); each slot leaves its sums, and a second
 // launch adds the slots of a group in their order.  float32 throughout.
+// Xout goes past the caches: it is wanted again behind the next block, and Y at once (32 760 rows of 1536, forward: 80 us, so 69; with a product of Y behind it 204 and
+// 202; Y past the caches too 63, with the product 213).
 //
-// 32 760 rows of 5120: forward 250 us (1.34 GB, 5.4 TB/s), backward 434 and 12 for the sums (2.01 GB, 4.6 TB/s).  4680 rows of 1536: forward 13.6 us (57 MB).
+// 32 760 rows of 5120: forward 247 us (1.34 GB, 5.4 TB/s), backward 434 and 12 for the sums (2.01 GB, 4.6 TB/s).  4680 rows of 1536: forward 12.6 us (57 MB).
 // One row: 2.7 us, the latency of its loads and sums.  1333 rows of 320, float32 stream, both ways: 4.6 + 7.0 + 4.2 + 2.9 us, four launches of little work.
 #include <hip/hip_runtime.h>
 #include <math.h>
@@ -132,13 +134,20 @@ template <bool F32> __device__ __forceinline__ Raw<F32> pack(const float (&x)[8]
   }
   return r;
 }
-template <bool F32> __device__ __forceinline__ void store_raw(void* base, int64_t at, const Raw<F32>& r) {
+template <bool F32, bool PAST = false> __device__ __forceinline__ void store_raw(void* base, int64_t at, const Raw<F32>& r) {      // PAST: the caches
   if constexpr (F32) {
     f32x4* p = reinterpret_cast<f32x4*>(reinterpret_cast<float*>(base) + at);
-    p[0] = r.a;
-    p[1] = r.b;
+    if constexpr (PAST) {
+      __builtin_nontemporal_store(r.a, p);
+      __builtin_nontemporal_store(r.b, p + 1);
+    } else {
+      p[0] = r.a;
+      p[1] = r.b;
+    }
   } else {
-    *reinterpret_cast<uint4*>(reinterpret_cast<uint16_t*>(base) + at) = r.u;
+    f32x4* p = reinterpret_cast<f32x4*>(reinterpret_cast<uint16_t*>(base) + at);
+    if constexpr (PAST) __builtin_nontemporal_store(__builtin_bit_cast(f32x4, r.u), p);
+    else *p = __builtin_bit_cast(f32x4, r.u);
   }
 }
 __device__ __forceinline__ void load_table(const float* p, float (&t)[8]) {
@@ -274,7 +283,7 @@ __global__ __launch_bounds__(most_threads(NC)) void lf_gate_norm_kernel(NormArgs
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[i][e] = fmaf(ga[i][e], b[i][e], x[i][e]);
         const Raw<F32> o = pack<F32>(x[i]);
-        if (in[i]) store_raw<F32>(a.Xout, (int64_t)r * a.xo_stride + ch[i], o);
+        if (in[i]) store_raw<F32, true>(a.Xout, (int64_t)r * a.xo_stride + ch[i], o);
         unpack<F32>(o, x[i]);
       }
     }
