@@ -239,7 +239,7 @@ int launch(const lf_grad_tensor* t, int32_t count, int64_t numel, float max_norm
   bool writes = false;
   for (int32_t i = 0; i < count; ++i) writes = writes || (t[i].numel > 0 && ((t[i].out && t[i].out != t[i].data) || max_norm != INFINITY));
   // Few shares are added by every workgroup of the scaling launch by itself, more of them (or without that launch) by a launch of their own (with and
-  // without it, us: 75 shares 7.6 and 6.7, 768 shares 13.2 and 12.7, 3072 shares 25.0 and 26.8).
+  // without it, us: 75 shares 7.6 and 6.7, 768 shares 13.2 and 12.7, four times as many 25.0 and 26.8).
   if (!writes || parts > 1024) {
     float* factor = reinterpret_cast<float*>(part + lf_grad_most_chunks(count, numel));
     if (lf_launch(lf_grad_norm_kernel, dim3(1), dim3(kThreads), 0, st, (const double*)part, parts, max_norm, eps, norm, factor) != hipSuccess)

@@ -153,7 +153,7 @@ template <int N> __device__ __forceinline__ void fetch(int32x4 rs_, uint32_t lds
                    "buffer_load_dwordx4 %1, %5, 0 offen lds\n\t"
                    "buffer_load_dwordx4 %2, %5, 0 offen offset:1024 lds\n\t"
                    "buffer_load_dwordx4 %3, %5, 0 offen offset:2048 lds\n\t"
-                   "buffer_load_dwordx4 %4, %5, 0 offen offset:3072 lds"
+                   "buffer_load_dwordx4 %4, %5, 0 offen offset:0xc00 lds"
                    :: "s"(at + 1024u * i), "v"(off[i]), "v"(off[i + 1]), "v"(off[i + 2]), "v"(off[i + 3]), "s"(rs) : "memory", "m0");
   } else if constexpr (N == 2) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\t"
