@@ -581,7 +581,7 @@ int lf_gate_norm_bwd(const void* Xout, const void* B, const float* gate, const f
  *   lse2_x = log2 sum_y exp2(q_x . k_y * softmax_scale * log2 e)   (+inf for a row that sees nothing).
  * lf_packed_attn_bwd computes dQ, dK and dV as lf_sparse_attn_bwd does, the sums running over what the rows see and, for dK and dV, over the heads
  * that share the head.  bf16 MFMA products with float32 accumulation, float32 online softmax; P and P (dP - delta) are rounded to bfloat16 before the
- * accumulating products (calls of few rows keep 16 bits of P); sums in a fixed order (no atomics: results are reproducible); bfloat16 outputs.  A long axis
+ * accumulating products (calls of few rows keep 16 bits of P; the P inside P (dP - delta) may have been rounded to 2^-10 of its value, however small); sums in a fixed order (no atomics: results are reproducible); bfloat16 outputs.  A long axis
  * is divided among workgroups where there are few rows and joined in a fixed order, so a row may differ between calls of other sizes by the order of sums.
  * Rows and tokens before the first and behind the last sequence are not looked at, and what is written leaves them as they were.
  * Arguments

@@ -11,7 +11,19 @@ namespace {
 
 constexpr int kTile = 32;         // streamed rows of a step
 
-typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+// Two probabilities on their way to another wavefront, in 32 bits.  0 <= P <= 1 has neither a sign nor the upper bit of the exponent; 16 bits hold the other seven of
+// that and nine of the fraction, so P is off by half a step, 2^-10 of the value, down to 2^-126.  (In binary16 what lies below 2^-14 has fewer bits and what lies below 2^-25
+// none: beside a token whose logits are 16 above theirs the others' dK was off by 2.8e-2 in the median, so by 2.6e-3.  In bfloat16 dK of 1333 tokens is off by 2.9e-3, so by 2.4e-3.)
+__device__ __forceinline__ uint32_t hand_over(float p0, float p1) {
+  const uint32_t lo = (__float_as_uint(p0) << 2) + 0x8000u, hi = (__float_as_uint(p1) << 2) + 0x8000u;
+  return __builtin_amdgcn_perm(hi, lo, 0x07060302u);
+}
+__device__ __forceinline__ float taken_over(uint32_t pair, int which) {
+  if (which) return __uint_as_float(pair >> 16 << 14);
+  uint32_t w;          // (pair & 0xffff) << 14, in one instruction
+  asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:WORD_0" : "=v"(w) : "v"(14), "v"(pair));
+  return __uint_as_float(w);
+}
 
 // One swizzle for tiles that are read both ways (rows, and transposed: half a wavefront takes four chunks of each of four rows); the transposing
 // read of rows 8 .. 15 of 16 sees chunk bit 1 flipped.
@@ -193,8 +205,7 @@ __global__ __launch_bounds__(256, 2) void lf_packed_dq_kernel(PackedArgs a) {
 }
 
 // dK and dV of 64 tokens: wavefront (rh, role) has 32 of them.  Role 0 computes S = Q K^T, P and dV^T += dO^T P, role 1 dP = dO V^T, dS and
-// dK^T += Q^T dS a step later, with the P that its partner has left in LDS (as binary16: P is 1 at the
-// most, and dS, which is rounded to bfloat16 again, has only half a step of that to bear); so one barrier a step is enough.  A tile is
+// dK^T += Q^T dS a step later, with the P that its partner has left in LDS (see hand_over); so one barrier a step is enough.  A tile is
 // requested two steps ahead; its Q lives for two steps (four stages), its dO for one (three).  SPLIT > 1: the workgroup holds SPLIT such groups with stages of their own, each takes a share of the steps (all the same number; those past
 // the end are empty), and their sums are added through LDS in order: for calls with too few tokens to fill the chip.
 // 1333 tokens in 9 sequences, 6 heads on 2 of 64: 19 us, 32 with tiles one step ahead and an LDS layout for the transposed reads alone: latency, a step after another.
@@ -223,7 +234,7 @@ __global__ __launch_bounds__(256 * SPLIT, SPLIT == 1 ? 2 : 1) void lf_packed_dkv
   if (tile < 0 || j0 >= s.nk) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((threadIdx.x >> 6) & 3);
   const int ln = lane & 31, kg = lane >> 5, rh = wave & 1;
-  const bool is_ds = wave >= 2;
+  const bool is_ds = (wave >= 2) != ((group & 1) != 0);      // every SIMD has as many wavefronts of either role
   const int j = j0 + 32 * rh + ln;
   const bool ok = j < s.nk;
   const int64_t token = (int64_t)s.k0 + j;
@@ -345,22 +356,23 @@ __global__ __launch_bounds__(256 * SPLIT, SPLIT == 1 ? 2 : 1) void lf_packed_dkv
       }
     }
     bf16x8 pf[2];
-    f16x8 ps[2];
+    u32x4 ps[2];
+    float p[16];
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-      const float p = __builtin_amdgcn_exp2f(sc[e] * a.c);
-      pf[e >> 3][e & 7] = (__bf16)p;
-      ps[e >> 3][e & 7] = (_Float16)p;
+      p[e] = __builtin_amdgcn_fmed3f(__builtin_amdgcn_exp2f(sc[e] * a.c), 0.0f, 1.0f);      // (lse2 is of rounded terms: P may come out as 1 + 2^-8)
+      pf[e >> 3][e & 7] = (__bf16)p[e];
+      if (e & 1) ps[e >> 3][(e & 7) >> 1] = hand_over(p[e - 1], p[e]);
     }
-    ph[t & 1][rh][0][lane] = __builtin_bit_cast(u32x4, ps[0]);
-    ph[t & 1][rh][1][lane] = __builtin_bit_cast(u32x4, ps[1]);
+    ph[t & 1][rh][0][lane] = ps[0];
+    ph[t & 1][rh][1][lane] = ps[1];
     accumulate(obuf[at], tf, pf);
   };
   // the one row that sees a single token (all rows of a sequence of one token do): see the dQ kernel
   const int lone = a.unit == 1 ? s.nq - s.nk : -1;
   // role 1, step t + 1: dS and dK of step t's rows [i, i + 32)
   auto ds_step = [&](int t, int i, f32x16 dp) __attribute__((always_inline)) {
-    const f16x8 pf[2] = {__builtin_bit_cast(f16x8, ph[t & 1][rh][0][lane]), __builtin_bit_cast(f16x8, ph[t & 1][rh][1][lane])};
+    const u32x4 ps[2] = {ph[t & 1][rh][0][lane], ph[t & 1][rh][1][lane]};
     bf16x8 tf[MB];
     first_half(qbuf[t & 3], tf);
     __builtin_amdgcn_sched_barrier(0);
@@ -373,7 +385,7 @@ __global__ __launch_bounds__(256 * SPLIT, SPLIT == 1 ? 2 : 1) void lf_packed_dkv
     }
     bf16x8 ds[2];
 #pragma unroll
-    for (int e = 0; e < 16; ++e) ds[e >> 3][e & 7] = (__bf16)((float)pf[e >> 3][e & 7] * dp[e]);
+    for (int e = 0; e < 16; ++e) ds[e >> 3][e & 7] = (__bf16)(taken_over(ps[e >> 3][(e & 7) >> 1], e & 1) * dp[e]);
     accumulate(qbuf[t & 3], tf, ds);
   };
   int wi = wi0;               // rows of the present step
@@ -430,7 +442,7 @@ __global__ __launch_bounds__(256 * SPLIT, SPLIT == 1 ? 2 : 1) void lf_packed_dkv
     constexpr int N = MB * 4 * 64;
     static_assert((SPLIT - 1) * 4 * N <= SPLIT * 7 * T32, "the sums fit the stages");
     f32x4* const sums = reinterpret_cast<f32x4*>(&buf_all[0][0][0]);
-    f32x4* const mine = sums + ((group - 1) * 4 + wave) * N;
+    f32x4* const mine = sums + ((group - 1) * 4 + 2 * is_ds + rh) * N;
     __syncthreads();
     if (group > 0) {
 #pragma unroll
@@ -442,7 +454,7 @@ __global__ __launch_bounds__(256 * SPLIT, SPLIT == 1 ? 2 : 1) void lf_packed_dkv
     if (group > 0) return;
 #pragma unroll
     for (int o = 1; o < SPLIT; ++o) {
-      const f32x4* theirs = sums + ((o - 1) * 4 + wave) * N;
+      const f32x4* theirs = sums + ((o - 1) * 4 + 2 * is_ds + rh) * N;
 #pragma unroll
       for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
