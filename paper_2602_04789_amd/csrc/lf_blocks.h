@@ -28,7 +28,8 @@ struct lf_norm_slots {
 lf_norm_slots lf_norm_bwd_slots(const lf_norm_shape* s);
 
 struct lf_norm_call {
-  const lf_norm_shape* s;
+  const lf_norm_shape* s;            // backward: with the groups that have tokens
+  int32_t groups;                    // backward: rows of the tables' gradients
   const void *X, *B;
   const float *gate, *post_weight, *weight, *scale, *shift;
   const int32_t* starts;

@@ -597,6 +597,7 @@ __global__ __launch_bounds__(FORM == kWide ? 1024 : 256) void lf_gate_norm_bwd_k
 
 struct SumArgs {
   NormArgs n;
+  int groups;            // of the tables: those past n.groups have no tokens
   float *dgate, *dscale, *dshift;
   float* sums;           // [groups][2][C]: S and T, for the weights; or null
   float *dweight, *dpost;
@@ -609,7 +610,7 @@ __global__ __launch_bounds__(16 * kSumRows) void lf_gate_norm_sum_kernel(SumArgs
   const NormArgs& a = b.n;
   __shared__ float s[3][kSumRows][17];
   const int col = threadIdx.x & 15, c = blockIdx.x * 16 + col, row = threadIdx.x >> 4;
-  for (int g = blockIdx.y; g < a.groups; g += gridDim.y) {
+  for (int g = blockIdx.y; g < b.groups; g += gridDim.y) {
     int64_t first, many;
     if (a.group_len > 0) {
       const int64_t rows = min((int64_t)a.group_len, (int64_t)a.L - (int64_t)g * a.group_len);
@@ -644,18 +645,19 @@ __global__ __launch_bounds__(16 * kSumRows) void lf_gate_norm_sum_kernel(SumArgs
 #pragma unroll
       for (int i = 0; i < kSumRows; ++i) t += s[row][i][col];
       const int64_t at = (int64_t)g * a.C + c;
+      const bool has = g < a.groups, only = has && a.groups == 1;
       if (c < a.C) {
         if (row == 0) {
           if (b.dscale) b.dscale[at] = a.weight ? t * a.weight[c] : t;
-          if (a.groups == 1 && b.dweight) b.dweight[c] = a.scale ? (1.0f + a.scale[c]) * t : t;
-          else if (b.sums) b.sums[2 * (int64_t)g * a.C + c] = t;
+          if (only && b.dweight) b.dweight[c] = a.scale ? (1.0f + a.scale[c]) * t : t;
+          else if (b.sums && has) b.sums[2 * (int64_t)g * a.C + c] = t;
         } else if (row == 1) {
           if (b.dshift) b.dshift[at] = t;
         } else {
           t *= a.rs;
           if (b.dgate) b.dgate[at] = a.post ? t * a.post[c] : t;
-          if (a.groups == 1 && b.dpost) b.dpost[c] = a.gate ? a.gate[c] * t : t;
-          else if (b.sums) b.sums[(2 * (int64_t)g + 1) * a.C + c] = t;
+          if (only && b.dpost) b.dpost[c] = a.gate ? a.gate[c] * t : t;
+          else if (b.sums && has) b.sums[(2 * (int64_t)g + 1) * a.C + c] = t;
         }
       }
     }
@@ -740,9 +742,9 @@ int lf_launch_gate_norm_bwd(const lf_norm_call* c, void* stream) {
   if (lf_launch(kernel, dim3((unsigned)n.slots), dim3(n.waves ? 256 : n.lay.threads), 0, st, a) != hipSuccess) return LF_ERR_HIP;
   if (!sums) return LF_OK;
   const bool weights = a.groups > 1 && (c->dweight || c->dpost_weight), many = n.slots > 64 * (int64_t)a.groups;
-  const SumArgs b = {a, c->dgate, c->dscale, c->dshift, weights ? c->workspace + n.slots * 3 * a.C : nullptr, c->dweight, c->dpost_weight};
+  const SumArgs b = {a, c->groups, c->dgate, c->dscale, c->dshift, weights ? c->workspace + n.slots * 3 * a.C : nullptr, c->dweight, c->dpost_weight};
   const unsigned across = (unsigned)(a.C + 15) / 16;
-  const dim3 grid(across, (unsigned)(a.groups < 4096 ? a.groups : 4096));
+  const dim3 grid(across, (unsigned)(c->groups < 4096 ? c->groups : 4096));
   if ((many ? lf_launch(lf_gate_norm_sum_kernel<64>, grid, dim3(1024), 0, st, b) : lf_launch(lf_gate_norm_sum_kernel<16>, grid, dim3(256), 0, st, b)) != hipSuccess)
     return LF_ERR_HIP;
   if (!weights) return LF_OK;
