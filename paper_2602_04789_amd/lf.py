@@ -591,6 +591,12 @@ def _int32(*values):
     return values
 
 
+def _small(sizes: int):
+    """_int32 for sizes of tensors, which are not negative, joined by `or` (0.1 us for all of them)."""
+    if sizes > 0x7FFFFFFF:
+        raise ValueError("a size or place does not fit 32 bits")
+
+
 def _size_of(query, make, *values) -> int:
     """What a size query of the library says of the structure that `make` builds from whole numbers, 0 where one does not fit."""
     try:
@@ -882,6 +888,7 @@ def _norm_groups(L: int, group_len: int, starts, at: int):
         if starts.dim() != 1 or starts.shape[0] < 2:
             raise ValueError("starts must be [groups + 1]")
         groups = starts.shape[0] - 1
+        _small(groups)
         return groups, 0, _vector(starts, groups + 1, (_torch or _get_torch()).int32, at, "starts")
     raise ValueError("groups are given by group_len > 0 or by starts")
 
@@ -897,6 +904,7 @@ def lf_gate_norm(X, B=None, gate=None, post_weight=None, weight=None, scale=None
     if len(rows) != 2 or dtype not in (_stream_dtypes or _dtypes()):
         raise ValueError("X must be bfloat16 or float32 [L, C]")
     L, n = rows
+    _small(L | n)
     at, st = _here(stream)
     groups, group_len, starts_ptr = _norm_groups(L, group_len, starts, at)
     xs = _row_stride(X, rows, dtype, at, "X")
@@ -948,6 +956,7 @@ def lf_gate_norm_bwd(Xout, dY, dXout=None, B=None, gate=None, post_weight=None, 
     if len(rows) != 2 or dtype not in (_stream_dtypes or _dtypes()):
         raise ValueError("Xout must be bfloat16 or float32 [L, C]")
     L, n = rows
+    _small(L | n)
     at, st = _here(stream)
     groups, group_len, starts_ptr = _norm_groups(L, group_len, starts, at)
     xos = _row_stride(Xout, rows, dtype, at, "Xout")
@@ -1013,7 +1022,8 @@ def _packed(Q, K, V, O, q_start, kv_start, causal):
     if q_start.dtype is not i32 or kv_start.dtype is not i32 or len(n) != 1 or n[0] < 2 or kv_start.shape != n or not q_start.is_contiguous() \
             or not kv_start.is_contiguous():
         raise ValueError("q_start and kv_start must be contiguous int32 [seqs + 1]")
-    causal, q_len, kv_len = _int32(causal, q_len, kv_len)
+    causal, = _int32(causal)
+    _small(heads | kv_heads | d | q_len | kv_len | n[0] - 1)
     return lf_packed_shape(heads, kv_heads, d, n[0] - 1, q_len, kv_len, causal, LF_BF16, qt, qh, kt, kh, vt, vh, ot, oh)
 
 
