@@ -541,7 +541,7 @@ int lf_token_attn_kvq(const void* Q, const void* cache, size_t cache_bytes, cons
  *   B, dB      device, bfloat16, row stride b_stride.       Y, dY   device, bfloat16, row stride y_stride.
  *   gate, scale, shift    device, float32 [groups][channels] with their row strides.   dgate, dscale, dshift   float32 [groups][channels], contiguous.
  *   post_weight, weight, dpost_weight, dweight   device, float32 [channels].
- *   workspace  device scratch of >= lf_gate_norm_bwd_workspace_bytes(), 256-byte aligned.
+ *   workspace  device scratch of >= lf_gate_norm_bwd_workspace_bytes(), 256-byte aligned.  Calls that may overlap must not share it.
  *   All pointers 16-byte aligned (starts: 4), row strides at least channels and multiples of 8 (tables: of 4; with one group any).  Outputs overlap nothing else.
  *   eps may be 0 (a token whose channels are all alike then gives NaN).
  * Errors: LF_ERR_NULL (also gate, post_weight or dB without B, B without Xout; a gradient of what the call does not have); LF_ERR_SHAPE (tokens not in 1 .. 2^30,
@@ -581,7 +581,8 @@ int lf_gate_norm_bwd(const void* Xout, const void* B, const float* gate, const f
  *   lse2_x = log2 sum_y exp2(q_x . k_y * softmax_scale * log2 e)   (+inf for a row that sees nothing).
  * lf_packed_attn_bwd computes dQ, dK and dV as lf_sparse_attn_bwd does, the sums running over what the rows see and, for dK and dV, over the heads
  * that share the head.  bf16 MFMA products with float32 accumulation, float32 online softmax; P and P (dP - delta) are rounded to bfloat16 before the
- * accumulating products (calls of few rows keep 16 bits of P; the P inside P (dP - delta) may have been rounded to 2^-10 of its value, however small); sums in a fixed order (no atomics: results are reproducible); bfloat16 outputs.  A long axis
+ * accumulating products (P keeps 16 bits in forward calls with q_len heads / kv_heads <= 16 seqs; the P inside
+ * P (dP - delta) may have been rounded to 2^-10 of its value, however small); sums in a fixed order (no atomics: results are reproducible); bfloat16 outputs.  A long axis
  * is divided among workgroups where there are few rows and joined in a fixed order, so a row may differ between calls of other sizes by the order of sums.
  * Rows and tokens before the first and behind the last sequence are not looked at, and what is written leaves them as they were.
  * Arguments
@@ -630,7 +631,7 @@ int lf_packed_attn_bwd(const void* Q, const void* K, const void* V, const void* 
  *              aligned to their element.  out = NULL: in place, and out_dtype is not looked at.  What is written overlaps no other
  *              tensor: a gradient that is listed twice is refused, unless the norm alone is taken.  numel may be 0.
  *   norm       device, float32, one element, written (infinity above 3.4e38).
- *   workspace  device scratch of >= lf_grad_workspace_bytes(count, sum of all numel), 256-byte aligned.
+ *   workspace  device scratch of >= lf_grad_workspace_bytes(count, sum of all numel), 256-byte aligned.  Calls that may overlap must not share it.
  * Errors: LF_ERR_NULL; LF_ERR_SHAPE (count not in 0 .. 2^20, numel negative, more than 2^40 elements in all, max_norm or eps negative or NaN, eps infinite,
  *   a tensor that is written and overlaps another); LF_ERR_DTYPE;
  *   LF_ERR_ALIGN; LF_ERR_WORKSPACE; LF_ERR_HIP.

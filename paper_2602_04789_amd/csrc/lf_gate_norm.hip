@@ -16,7 +16,7 @@
 // 202; Y past the caches too 63, with the product 213).
 //
 // 32 760 rows of 5120: forward 247 us (1.34 GB, 5.4 TB/s), backward 434 and 12 for the sums (2.01 GB, 4.6 TB/s).  4680 rows of 1536: forward 12.6 us (57 MB).
-// One row: 2.7 us, the latency of its loads and sums.  1333 rows of 320, float32 stream, both ways: 4.6 + 7.0 + 4.2 + 2.9 us, four launches of little work.
+// 4680 rows of 8192: forward 56 us, float32 stream 195 (96 registers spill; 94 at 4.9 TB/s).  One row: 2.7 us, the latency of its loads and sums.  1333 rows of 320, float32 stream, both ways: 4.6 + 7.0 + 4.2 + 2.9 us, four launches of little work.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -355,7 +355,8 @@ __device__ __forceinline__ Slot find_slot(const NormArgs& a, int64_t s) {
 //   kRow      one at a time, the next two on their way
 //   kWaves    one for each of its four wavefronts (narrow rows: no barrier, and the four leave one set of sums)
 //   kWide     one at a time, for rows of more than 6 144 channels: values stay packed and are unpacked where they are used, tables are read from
-//             memory, and nothing is on its way, so that the sums fit the registers of 1 024 threads
+//             memory, and nothing is on its way.  All the same 128 registers, as 1 024 threads have, are too few: 86 to 172 spill, and scratch bounds
+//             it (4680 rows of 8192 399 us, with post_weight 688, 94 at 4.9 TB/s; of 16 384 589 and 1090, 188)
 enum NormForm { kRow, kWaves, kWide };
 
 template <int NC, bool F32, int FORM, bool POST>

@@ -488,13 +488,15 @@ template <int D> int launch(const PackedArgs& a, hipStream_t st) {
   }
   if (a.kv_len == 0) return LF_OK;
   // 256 tokens of a workgroup with 112 of them or more; where rows see the tokens ahead of them only, so that the first workgroups work longest, 352
-  // (both gradients, us, with them and with the better of the two below: 12 heads of 2048 tokens 205 and 177, 2731 305 and 324; causal, 32 heads on 4 of
-  // 16 384 tokens 11 406 and 9994, 24 000 20 164 and 20 673; by chunks of 512, 12 heads of 4096 378 and 327, 8192 911 and 951).
+  // (both gradients, us, with them and with the better of the two below: 12 heads of 2048 tokens 161 and 136, 2731 230 and 255; causal, 32 heads on 4 of
+  // 16 384 tokens 9195 and 8191, 24 000 15 871 and 16 815; by chunks of 512, 12 heads of 4096 304 and 252, 8192 697 and 746).  Those are single sequences.  Short ones
+  // leave wavefronts of 64 tokens without any, which the rule does not look at (12 heads, 100 sequences of 300 tokens 464 and 407, 500 of 64 357 and 262).
   if (D == 128 && (int64_t)a.kv_len * a.Hk >= 256 * (a.unit ? 352 : 112)) return lf_launch_packed_dkv_wide(a, st);
   constexpr int kSplit = D == 128 ? 2 : 4;       // groups that a compute unit's LDS has room for
   const int64_t blocks = (int64_t)(a.kv_len / 64 + a.seqs) * a.Hk;
-  // several groups to a workgroup while a compute unit has two of them or fewer (divided and not: 32 heads on 4 of 128, 8192 tokens, causal 2451 and
-  // 2916, 12 000 tokens 5675 and 5548; 8 heads of 64, 2048 tokens 97 and 110; 256 sequences of 200 tokens, 8 heads on 2 of 64, 241 and 193)
+  // several groups to a workgroup while a compute unit has two of them or fewer (divided and not: 32 heads on 4 of 128, 8192 tokens, causal 2174 and
+  // 2513, 12 000 tokens 4710 and 4384; 8 heads of 64, 2048 tokens, causal 67 and 81; 256 sequences of 200 tokens, 8 heads on 2 of 64, 239 and 197; but 12 heads of 128, 2048
+  // tokens, 144 and 136).  Few tokens under many rows leave compute units without work either way (12 heads, 32 760 rows over 512 tokens 725 and 926).
   const bool split = (int64_t)(a.kv_len / 64 + a.seqs - 1) * a.Hk <= 2 * 256;
   const hipError_t rc = split ? lf_launch(lf_packed_dkv_kernel<D, kSplit>, dim3((unsigned)blocks), dim3(256 * kSplit), 0, st, a)
                               : lf_launch(lf_packed_dkv_kernel<D, 1>, dim3((unsigned)blocks), dim3(256), 0, st, a);
